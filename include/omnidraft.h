@@ -132,7 +132,14 @@ enum od_counter {
 #define OD_TAU_SAMPLE 2.0e-6
 #define OD_TAU_EXIT 4.0e-6f
 
+/* flags[b,r] written by od_token_logprobs */
+#define OD_LF_BAD_TEMPERATURE 0x1u /* not positive and finite: nothing of the row was read */
+#define OD_LF_NONFINITE 0x2u       /* the row holds NaN or +inf: its results are NaN */
+#define OD_LF_NO_MASS 0x4u         /* every logit of the row is -inf */
+#define OD_LF_BAD_ID 0x8u          /* the given id is outside the vocabulary and not -1 */
+
 #define OD_MAX_K 16      /* largest K_max */
+#define OD_MAX_TOP 32    /* od_token_logprobs: most alternatives of a row */
 #define OD_NOALLOC_MAX_ROWS 1024 /* od_verify_noalloc: largest B * (K_max + 1) */
 #define OD_NGRAM_MAX 4   /* longest cached run */
 
@@ -384,6 +391,63 @@ int32_t od_distill_loss(od_ctx *ctx, int32_t B, int32_t K_max, const float *q_ro
                         const float *row_sum, const float *p_sel,
                         const float *temperature, float lambda, int32_t lambda_mode,
                         float *loss, float *grad, void *stream);
+
+/* ---- scores of tokens ----------------------------------------------------- */
+
+/* The log probability of one given token, the entropy and the likeliest tokens of each
+ * logit row: what a server returns beside the tokens that it verified, and what a loss on
+ * likelihood or entropy is made of. Of either model: `vocab` is the length of a row (any,
+ * not bound to the context's vocabularies), B and R are not bound to its batch; no
+ * vocabulary map is needed. Row (b, r), p = softmax(x / T_b):
+ *   logprob = ln p(ids[b,r]); entropy = -sum_t p(t) ln p(t);
+ *   top_ids, top_logprobs = the n_top largest logits in order, equal ones by the lower id.
+ * A row is read once (its largest elements are looked at again).
+ *   in  (device) logits  fp32 or bf16, element (b, r, t) at b*seq_stride + r*row_stride + t
+ *                        (strides in elements; base and both strides multiples of 16 bytes);
+ *                        nothing beyond a row's vocab elements is read
+ *                ids         int32[B,R], -1 = none (NULL = none anywhere)
+ *                n_rows      int32[B]: rows r < n_rows[b] count (NULL = all R); of others
+ *                            nothing is read and nothing is written
+ *                temperature float[B], positive and finite, its reciprocal too (NULL = 1)
+ *   out (device) logprob float[B,R] (0 where no id is given), entropy float[B,R],
+ *                flags uint32[B,R] (OD_LF_*) (any of the three may be NULL);
+ *                row_max, row_sum float[B,R]: max_t x_t and sum_t exp((x_t - row_max)/T_b), as
+ *                        od_verify writes them;
+ *                top_ids int32[B,R,n_top], top_logprobs float[B,R,n_top] (n_top in
+ *                        0..OD_MAX_TOP, NULL with 0); where fewer ids than n_top have a logit
+ *                        above -inf the rest is id -1 with -inf
+ * A row of nothing but -inf (NO_MASS): row_max and the log probability of a given id are -inf,
+ * row_sum and entropy 0, no alternatives. A row with NaN or +inf (NONFINITE): all NaN, ids -1. A bad
+ * temperature: all 0, no alternatives. An id outside the vocabulary counts as none (BAD_ID).
+ * Asynchronous on `stream`; no scratch, so calls on one context need no order among them. */
+int32_t od_token_logprobs(od_ctx *ctx, int32_t B, int32_t R, int32_t vocab, const void *logits,
+                          int32_t logit_dtype, int64_t row_stride, int64_t seq_stride,
+                          const int32_t *ids, const int32_t *n_rows, const float *temperature,
+                          int32_t n_top, float *logprob, float *entropy, float *row_max,
+                          float *row_sum, int32_t *top_ids, float *top_logprobs,
+                          uint32_t *flags, void *stream);
+
+/* The gradient of those results with respect to the logits, from the gradients of a loss with
+ * respect to them:
+ *   grad(t) = (1/T) (sum_i g_i [t == id_i] - p(t) (sum_i g_i + g_entropy (ln p(t) + entropy))),
+ * i over the given id (g_logprob) and the listed alternatives (g_top). An id that is
+ * named twice gets both; entries without an id take no part.
+ *   in  (device) logits, ids, n_rows, temperature as for od_token_logprobs; row_max, row_sum,
+ *                entropy, top_ids as it wrote them (entropy is needed with g_entropy, top_ids with
+ *                g_top); g_logprob, g_entropy float[B,R], g_top float[B,R,n_top] (any may be NULL = 0)
+ *   out (device) grad, of the logits' type, element (b, r, t) at b*grad_seq_stride +
+ *                r*grad_row_stride + t (alignment as for the logits); it may be the logits
+ *                themselves, with the same strides. Rows that do not count, with a bad
+ *                temperature or without mass are 0; nothing behind a row is written.
+ * Asynchronous on `stream`; no scratch. */
+int32_t od_token_logprobs_grad(od_ctx *ctx, int32_t B, int32_t R, int32_t vocab,
+                               const void *logits, int32_t logit_dtype, int64_t row_stride,
+                               int64_t seq_stride, const int32_t *ids, const int32_t *n_rows,
+                               const float *temperature, const float *row_max,
+                               const float *row_sum, const float *entropy, int32_t n_top,
+                               const int32_t *top_ids, const float *g_logprob,
+                               const float *g_entropy, const float *g_top, void *grad,
+                               int64_t grad_row_stride, int64_t grad_seq_stride, void *stream);
 
 /* Adaptive drafting, exit rule (Section 3.3, Eq. (4)-(6)). From the acceptance
  * head's outputs f_phi(e_i) of the proposed tokens:

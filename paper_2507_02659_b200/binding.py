@@ -33,13 +33,16 @@ OD_CNT_COUNT = 4
 OD_VF_BOUNDARY_MASK, OD_VF_BAD_TEMPERATURE, OD_VF_NONFINITE = 0xFFFF, 0x10000, 0x20000
 OD_SF_BOUNDARY, OD_SF_ZERO_MASS, OD_SF_BAD_TEMPERATURE, OD_SF_BONUS = 0x1, 0x2, 0x4, 0x10
 OD_TAU_ACCEPT, OD_TAU_SAMPLE, OD_TAU_EXIT = 1.0e-5, 2.0e-6, 4.0e-6
+OD_LF_BAD_TEMPERATURE, OD_LF_NONFINITE, OD_LF_NO_MASS, OD_LF_BAD_ID = 0x1, 0x2, 0x4, 0x8
 OD_MAX_K = 16
+OD_MAX_TOP = 32
 OD_NOALLOC_MAX_ROWS = 1024
 
 EXPORTS = ["od_create", "od_destroy", "od_set_vocab_map", "od_cache_build", "od_set_option",
            "od_map_proposals", "od_verify", "od_sample_residual", "od_step", "od_host_step_reserve",
            "od_step_host", "od_verify_noalloc", "od_exit_rule", "od_cache_configure", "od_cache_set_clock",
            "od_cache_insert", "od_cache_trim", "od_cache_dump", "od_cache_stats", "od_distill_loss",
+           "od_token_logprobs", "od_token_logprobs_grad",
            "od_verify_shard_stats", "od_verify_shard_finish", "od_sample_shard_mass", "od_sample_shard_pick",
            "od_last_launch_info", "od_status_string", "od_version"]
 
@@ -79,6 +82,9 @@ def lib():
         L.od_exit_rule.argtypes = [vp, i32, i32, vp, vp, C.c_float, vp, vp, vp, vp]
         L.od_distill_loss.argtypes = ([vp, i32, i32] + [vp] * 7 + [i32, i64, i64] + [vp] * 4
                                       + [C.c_float, i32, vp, vp, vp])
+        L.od_token_logprobs.argtypes = [vp, i32, i32, i32, vp, i32, i64, i64, vp, vp, vp, i32] + [vp] * 7 + [vp]
+        L.od_token_logprobs_grad.argtypes = ([vp, i32, i32, i32, vp, i32, i64, i64] + [vp] * 6 + [i32] + [vp] * 5
+                                             + [i64, i64, vp])
         L.od_verify_shard_stats.argtypes = [vp, i32, i32, i32, i32, vp, i32, i64, i64] + [vp] * 4 + [vp]
         L.od_verify_shard_finish.argtypes = [vp, i32, i32, i32] + [vp] * 7 + [u64] + [vp] * 7 + [vp]
         L.od_sample_shard_mass.argtypes = [vp, i32, i32, i32, i32, vp, i32, i64, i64] + [vp] * 12 + [vp] + [vp]
@@ -397,6 +403,92 @@ def od_distill_loss(ctx: Context, q_rows, draft_ids, mp: MapOut, logits, vo: Ver
         _dp(vo.row_sum, f32, d), _dp(vo.p_sel, f32, d), _dp(temperature, f32, d), C.c_float(lam),
         int(lambda_mode), _dp(loss, f32, d), _dp(grad, f32, d), _stream(d)), "od_distill_loss")
     return loss, grad
+
+
+# ---- scores of tokens, and their gradient ----
+
+@dataclass
+class LogprobOut:
+    logprob: torch.Tensor
+    entropy: torch.Tensor
+    row_max: torch.Tensor
+    row_sum: torch.Tensor
+    top_ids: torch.Tensor
+    top_logprobs: torch.Tensor
+    flags: torch.Tensor
+
+
+def alloc_logprob_out(ctx: Context, B: int, R: int, n_top: int = 0) -> LogprobOut:
+    d = ctx.device
+    f = lambda *s: torch.zeros(*s, dtype=torch.float32, device=d)
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32, device=d)
+    return LogprobOut(f(B, R), f(B, R), f(B, R), f(B, R), i(B, R, n_top), f(B, R, n_top), i(B, R))
+
+
+def _row_strides(t: torch.Tensor, device, what: str):
+    """(B, R, V, row stride, sequence stride) of rows [B, R, V]."""
+    if t.dim() != 3 or t.shape[2] < 1 or t.shape[1] < 1:
+        raise ValueError(f"{what} must be [B, R, V], got {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{what} on another device")
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"rows of {what} must be dense")
+    B, R, V = t.shape
+    # (torch gives a dimension of one entry any stride)
+    esz = t.element_size()
+    row = int(t.stride(1)) if R > 1 else (int(t.stride(0)) if B > 1 else -(-V * esz // 16) * 16 // esz)
+    return B, R, V, row, int(t.stride(0)) if B > 1 else row * R
+
+
+def _shaped(t: Optional[torch.Tensor], shape, what: str):
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what} must be {list(shape)}, got {tuple(t.shape)}")
+    return t
+
+
+def od_token_logprobs(ctx: Context, logits, ids=None, temperature=None, n_rows=None, n_top: int = 0,
+                      out: Optional[LogprobOut] = None) -> LogprobOut:
+    """Log probability of ids [B, R] (-1 = none), entropy and the n_top likeliest tokens of logit rows [B, R, V]."""
+    d, i32, f32 = ctx.device, torch.int32, torch.float32
+    B, R, V, rs, ss = _row_strides(logits, d, "logits")
+    out = out or alloc_logprob_out(ctx, B, R, n_top)
+    for name, t in vars(out).items():
+        _shaped(t, (B, R, n_top) if name.startswith("top") else (B, R), name)
+    _shaped(ids, (B, R), "ids"); _shaped(temperature, (B,), "temperature"); _shaped(n_rows, (B,), "n_rows")
+    _check(lib().od_token_logprobs(
+        ctx.handle, B, R, V, C.c_void_p(logits.data_ptr()), logit_dtype_code(logits), rs, ss, _dp(ids, i32, d),
+        _dp(n_rows, i32, d), _dp(temperature, f32, d), n_top, _dp(out.logprob, f32, d), _dp(out.entropy, f32, d),
+        _dp(out.row_max, f32, d), _dp(out.row_sum, f32, d), _dp(out.top_ids, i32, d), _dp(out.top_logprobs, f32, d),
+        _dp(out.flags, i32, d), _stream(d)), "od_token_logprobs")
+    return out
+
+
+def od_token_logprobs_grad(ctx: Context, logits, ids, lp: LogprobOut, g_logprob=None, g_entropy=None, g_top=None,
+                           temperature=None, n_rows=None, grad=None):
+    """The gradient with respect to the logits from those of the log probabilities [B, R], the entropies [B, R]
+    and the alternatives' log probabilities [B, R, n]; grad may be the logits themselves."""
+    d, i32, f32 = ctx.device, torch.int32, torch.float32
+    B, R, V, rs, ss = _row_strides(logits, d, "logits")
+    if grad is None:
+        per = 16 // logits.element_size()
+        grad = torch.empty(B, R, -(-V // per) * per, dtype=logits.dtype, device=d)[:, :, :V]
+    if grad.dtype != logits.dtype or tuple(grad.shape) != (B, R, V):
+        raise ValueError("grad must have the logits' type and shape")
+    _, _, _, grs, gss = _row_strides(grad, d, "grad")
+    n = int(g_top.shape[2]) if g_top is not None else 0
+    for name, t in dict(ids=ids, g_logprob=g_logprob, g_entropy=g_entropy, row_max=lp.row_max, row_sum=lp.row_sum,
+                        entropy=lp.entropy).items():
+        _shaped(t, (B, R), name)
+    _shaped(temperature, (B,), "temperature"); _shaped(n_rows, (B,), "n_rows")
+    if g_top is not None:
+        _shaped(g_top, (B, R, n), "g_top"); _shaped(lp.top_ids, (B, R, n), "top_ids")
+    _check(lib().od_token_logprobs_grad(
+        ctx.handle, B, R, V, C.c_void_p(logits.data_ptr()), logit_dtype_code(logits), rs, ss, _dp(ids, i32, d),
+        _dp(n_rows, i32, d), _dp(temperature, f32, d), _dp(lp.row_max, f32, d), _dp(lp.row_sum, f32, d),
+        _dp(lp.entropy, f32, d), n, _dp(lp.top_ids, i32, d) if n else None, _dp(g_logprob, f32, d),
+        _dp(g_entropy, f32, d), _dp(g_top, f32, d), C.c_void_p(grad.data_ptr()), grs, gss, _stream(d)),
+        "od_token_logprobs_grad")
+    return grad
 
 
 def od_exit_rule(ctx: Context, head_logits, avail_len, gamma: float):

@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libomnidraft.so")
 EXT = os.path.join(HERE, "_marshal.so")
 EXT_FOR = os.path.join(HERE, "_build", "marshal_built_for")
-SOURCES = ["od_api.cu", "od_map.cu", "od_verify.cu", "od_sample.cu", "od_step.cu", "od_host.cu", "od_noalloc.cu", "od_exit.cu", "od_cache.cu", "od_distill.cu"]
+SOURCES = ["od_api.cu", "od_map.cu", "od_verify.cu", "od_sample.cu", "od_step.cu", "od_host.cu", "od_noalloc.cu", "od_exit.cu", "od_cache.cu", "od_distill.cu", "od_score.cu"]
 
 
 def _newest_source() -> float:
@@ -75,7 +75,7 @@ def _build_lib(force: bool = False, verbose: bool = False) -> str:
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     tmp = LIB + f".{os.getpid()}.tmp"
-    cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3",
+    cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-t", "0",
            "-std=c++17", "-shared", "-Xcompiler", "-fPIC", "-Xlinker", "-soname=libomnidraft.so", "-Xptxas", "-v",
            "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-o", tmp]
     cmd += [os.path.join(CSRC, s) for s in SOURCES]

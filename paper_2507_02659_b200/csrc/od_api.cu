@@ -86,6 +86,19 @@ int32_t check_logits(const od_ctx *c, const void *logits, int32_t dtype, int64_t
     return check_logits_len(c->v_p, logits, dtype, row_stride, seq_stride, K_max);
 }
 
+// rows of any vocabulary that are not tied to a step: B sequences of R rows
+int32_t check_rows(const od_ctx *c, int32_t B, int32_t R, int32_t vocab)
+{
+    if (!c || B < 0 || R < 1 || (int64_t)B * R > INT32_MAX) return OD_ERR_INVALID_ARG;
+    if (vocab < 1) return OD_ERR_INVALID_ARG;
+    return vocab <= (1 << 30) ? OD_OK : OD_ERR_UNSUPPORTED;
+}
+int32_t check_row_tensor(int32_t vocab, const void *rows, int32_t dtype, int32_t R, int64_t row_stride, int64_t seq_stride)
+{
+    if (R > 1 && row_stride > INT64_MAX / R) return OD_ERR_INVALID_ARG;
+    return check_logits_len(vocab, rows, dtype, row_stride, seq_stride, R - 1);
+}
+
 // a vocabulary shard: whole 256-id tiles, inside the vocabulary
 int32_t check_shard(const od_ctx *c, int32_t shard_lo, int32_t shard_len)
 {
@@ -630,6 +643,47 @@ int32_t od_exit_rule(od_ctx *c, int32_t B, int32_t K_max, const float *head_logi
     if (!g.ok) return OD_ERR_CUDA;
     OD_CUDA(od_launch_exit(B, K_max, head_logits, avail_len, gamma, draft_len, reject_prob, exit_flags, c->opt_pdl != 0,
                            (cudaStream_t)stream));
+    return OD_OK;
+}
+
+int32_t od_token_logprobs(od_ctx *c, int32_t B, int32_t R, int32_t vocab, const void *logits, int32_t logit_dtype,
+                          int64_t row_stride, int64_t seq_stride, const int32_t *ids, const int32_t *n_rows,
+                          const float *temperature, int32_t n_top, float *logprob, float *entropy, float *row_max,
+                          float *row_sum, int32_t *top_ids, float *top_logprobs, uint32_t *flags, void *stream)
+{
+    int32_t st = check_rows(c, B, R, vocab);
+    if (st != OD_OK || B == 0) return st;
+    st = check_row_tensor(vocab, logits, logit_dtype, R, row_stride, seq_stride);
+    if (st != OD_OK) return st;
+    if (n_top < 0 || n_top > OD_MAX_TOP || (n_top > 0 && (!top_ids || !top_logprobs))) return OD_ERR_INVALID_ARG;
+    if (!row_max || !row_sum) return OD_ERR_INVALID_ARG;
+    DeviceGuard g(c->device);
+    if (!g.ok) return OD_ERR_CUDA;
+    OD_CUDA(od_launch_score(c, B, R, vocab, logits, logit_dtype, row_stride, seq_stride, ids, n_rows, temperature, n_top, logprob,
+                            entropy, row_max, row_sum, top_ids, top_logprobs, flags, (cudaStream_t)stream));
+    return OD_OK;
+}
+
+int32_t od_token_logprobs_grad(od_ctx *c, int32_t B, int32_t R, int32_t vocab, const void *logits, int32_t logit_dtype,
+                               int64_t row_stride, int64_t seq_stride, const int32_t *ids, const int32_t *n_rows,
+                               const float *temperature, const float *row_max, const float *row_sum, const float *entropy,
+                               int32_t n_top, const int32_t *top_ids, const float *g_logprob, const float *g_entropy,
+                               const float *g_top, void *grad, int64_t grad_row_stride, int64_t grad_seq_stride, void *stream)
+{
+    int32_t st = check_rows(c, B, R, vocab);
+    if (st != OD_OK || B == 0) return st;
+    st = check_row_tensor(vocab, logits, logit_dtype, R, row_stride, seq_stride);
+    if (st == OD_OK) st = check_row_tensor(vocab, grad, logit_dtype, R, grad_row_stride, grad_seq_stride);
+    if (st != OD_OK) return st;
+    if (n_top < 0 || n_top > OD_MAX_TOP || !row_max || !row_sum) return OD_ERR_INVALID_ARG;
+    if ((g_top && (n_top == 0 || !top_ids)) || (g_entropy && !entropy)) return OD_ERR_INVALID_ARG;
+    if (grad == logits && (grad_row_stride != row_stride || grad_seq_stride != seq_stride)) return OD_ERR_INVALID_ARG;
+    if (od_score_grad_blocks((int64_t)B * R, vocab, logit_dtype) > INT32_MAX) return OD_ERR_UNSUPPORTED;
+    DeviceGuard g(c->device);
+    if (!g.ok) return OD_ERR_CUDA;
+    OD_CUDA(od_launch_score_grad(c, B, R, vocab, logits, logit_dtype, row_stride, seq_stride, ids, n_rows, temperature, row_max,
+                                 row_sum, entropy, n_top, top_ids, g_logprob, g_entropy, g_top, grad, grad_row_stride,
+                                 grad_seq_stride, (cudaStream_t)stream));
     return OD_OK;
 }
 

@@ -305,6 +305,17 @@ void od_distill_plan(int32_t v_q, int32_t v_p, const OdMappedIds &mapped, void *
 cudaError_t od_distill_prepare_device(int32_t v_q);
 void od_distill_resident(int32_t *clusters);             // [levels]
 
+cudaError_t od_launch_score(const od_ctx *c, int32_t B, int32_t R, int32_t V, const void *logits, int32_t dtype, int64_t row_stride,
+                            int64_t seq_stride, const int32_t *ids, const int32_t *n_rows, const float *temperature, int32_t n_top,
+                            float *logprob, float *entropy, float *row_max, float *row_sum, int32_t *top_ids, float *top_logprobs,
+                            uint32_t *flags, cudaStream_t s);
+int64_t od_score_grad_blocks(int64_t rows, int32_t V, int32_t dtype);   // of the launch below
+cudaError_t od_launch_score_grad(const od_ctx *c, int32_t B, int32_t R, int32_t V, const void *logits, int32_t dtype, int64_t row_stride,
+                                 int64_t seq_stride, const int32_t *ids, const int32_t *n_rows, const float *temperature,
+                                 const float *row_max, const float *row_sum, const float *entropy, int32_t n_top,
+                                 const int32_t *top_ids, const float *g_logprob, const float *g_entropy, const float *g_top, void *grad,
+                                 int64_t grad_row_stride, int64_t grad_seq_stride, cudaStream_t s);
+
 void od_cache_free_dynamic(od_ctx *c);   // frees what od_cache_configure allocated beyond keys / vals
 
 cudaError_t od_launch_exit(int32_t B, int32_t K_max, const float *head_logits, const int32_t *avail_len,

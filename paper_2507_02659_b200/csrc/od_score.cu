@@ -1,0 +1,554 @@
+// Scores of tokens from logit rows, and their gradient. For a row x of V logits at temperature T, with
+// M = max x, e_j = exp((x_j - M) / T), S = sum e, p = e / S:
+//   log probability   ln p_t = (x_t - M) / T - ln S
+//   entropy           H = ln S - (1 / S) sum_j e_j (x_j - M) / T
+//   alternatives      the n largest logits, equal ones by the lower id
+//   gradient          d/dx_j = (1/T) (sum_i g_i [j == id_i] - p_j (G + g_H (ln p_j + H))),  G = sum_i g_i,
+//                     i over the given token and the listed alternatives
+// Everything is held in fp32. Differences from the running maximum are formed before they are scaled: x T^-1 may
+// overflow (a mask of the type's lowest value) or lose the digits that the exponential is made of, x - M does not.
+//
+// Forward: one pass. A block of 256 threads (or a cluster of them: one contiguous slice of the row to each) keeps, per
+// thread, the maximum, the sum of e and the sum of e (x - M), raised to a new maximum once per four 16-byte loads.
+// The alternatives cost next to nothing in that pass: the largest logits of 32 groups of eight threads are 32 different
+// elements, so the n-th largest of them is a bound that at least n elements of the slice reach and few more do; only
+// the threads whose own maximum reaches it look at their elements again (from L2), and what reaches the bound is
+// ranked by counting.
+//
+// Backward: elementwise, one read and one write; the given token and the alternatives are written over the dense
+// values of their chunk behind a block barrier.
+#include <float.h>
+
+#include "od_common.cuh"
+
+namespace {
+
+constexpr int THREADS = 256;
+constexpr int WARPS = THREADS / 32;
+constexpr int GROUPS = THREADS / 8;                        // of eight threads
+constexpr int U = 4;                                       // 16-byte loads of a thread in flight
+constexpr int MAX_SPLIT = 8;                               // blocks of a row (a portable cluster)
+constexpr int CAP = 512;                                   // candidates that are ranked by counting
+constexpr float LEAST = -150.f;                            // exp2 of it is zero
+constexpr float LN2 = 0.69314718055994531f, LOG2E = 1.4426950408889634f;
+static_assert(GROUPS == 32, "a group to each lane");
+static_assert(WARPS * OD_MAX_TOP <= CAP && MAX_SPLIT * OD_MAX_TOP <= CAP, "a list from every warp, or block, fits");
+
+struct ScoreArgs {
+    const char *logits;
+    int64_t row_bytes, seq_bytes;
+    int32_t R, V, n_top, split;                            // blocks of a row
+    const int32_t *ids, *n_rows;
+    const float *temperature;
+    float *logprob, *entropy, *row_max, *row_sum, *top_logprobs;
+    int32_t *top_ids;
+    uint32_t *flags;
+};
+
+__device__ __forceinline__ uint4 ld_stream(const void *p)
+{
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t bf16x2_max(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
+template <int DTYPE> constexpr int VEC = DTYPE == OD_BF16 ? 8 : 4;
+template <int DTYPE> constexpr uint32_t NONE = DTYPE == OD_BF16 ? 0xFF80FF80u : 0xFF800000u;   // -inf
+
+template <int DTYPE>
+__device__ __forceinline__ float element(const uint4 &v, int k)
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    if (DTYPE == OD_F32) return __uint_as_float(w[k]);
+    return k & 1 ? od_bf16_hi(w[k >> 1]) : od_bf16_lo(w[k >> 1]);
+}
+
+// vector i of a row: whole ones as they lie; of a last one that the row ends in, what is there and -inf.
+// READ_ONLY: the kernel does not write the row
+template <int DTYPE, bool READ_ONLY = true>
+__device__ __forceinline__ uint4 load_vec(const char *row, int i, int V)
+{
+    if (i < V / VEC<DTYPE>) return READ_ONLY ? ld_stream(row + (size_t)i * 16) : __ldcs((const uint4 *)(row + (size_t)i * 16));
+    uint32_t w[4] = {NONE<DTYPE>, NONE<DTYPE>, NONE<DTYPE>, NONE<DTYPE>};
+#pragma unroll
+    for (int k = 0; k < VEC<DTYPE>; ++k) {
+        const int j = i * VEC<DTYPE> + k;
+        if (j >= V) continue;
+        if (DTYPE == OD_F32) w[k] = __ldcs((const uint32_t *)row + j);
+        else w[k >> 1] = (w[k >> 1] & (k & 1 ? 0xFFFFu : 0xFFFF0000u)) | (uint32_t)__ldcs((const unsigned short *)row + j) << (k & 1 ? 16 : 0);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// c = the largest logit so far (at least -FLT_MAX), s = sum of exp2((x - c) scale), a = sum of those times (x - c) scale
+struct Sums {
+    float c, s, a;
+    __device__ __forceinline__ void raise(float to, float scale)
+    {
+        const float cn = fmaxf(c, to), d = fmaxf((c - cn) * scale, LEAST), f = od_ex2(d);
+        a = (a + s * d) * f;
+        s *= f;
+        c = cn;
+    }
+};
+
+__device__ __forceinline__ void absorb_pair(uint64_t &s2, uint64_t &a2, float lo, float hi, uint64_t nc2, uint64_t scale2)
+{
+    float d0, d1;
+    f2_unpack(f2_mul(f2_add(f2_pack(lo, hi), nc2), scale2), d0, d1);
+    const uint64_t e2 = f2_pack(od_ex2(d0), od_ex2(d1));
+    s2 = f2_add(s2, e2);
+    // (an exponential of -inf is zero, and so is its product with what is clamped here; NaN is in e)
+    a2 = f2_fma(e2, f2_pack(fmaxf(d0, LEAST), fmaxf(d1, LEAST)), a2);
+}
+
+template <int DTYPE>
+__device__ __forceinline__ void absorb(Sums &t, const uint4 (&x)[U], float scale)
+{
+    float gm;
+    if (DTYPE == OD_BF16) {
+        uint32_t g = NONE<DTYPE>;
+#pragma unroll
+        for (int u = 0; u < U; ++u) g = bf16x2_max(bf16x2_max(bf16x2_max(g, x[u].x), bf16x2_max(x[u].y, x[u].z)), x[u].w);
+        gm = fmaxf(od_bf16_lo(g), od_bf16_hi(g));
+    } else {
+        gm = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            gm = fmaxf(gm, fmaxf(fmaxf(__uint_as_float(x[u].x), __uint_as_float(x[u].y)),
+                                 fmaxf(__uint_as_float(x[u].z), __uint_as_float(x[u].w))));
+    }
+    t.raise(gm, scale);
+    const uint64_t nc2 = f2_pack(-t.c, -t.c), scale2 = f2_pack(scale, scale);
+    uint64_t s0 = 0, s1 = 0, a0 = 0, a1 = 0;               // pairs of zeros
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int k = 0; k < VEC<DTYPE>; k += 4) {
+            absorb_pair(s0, a0, element<DTYPE>(x[u], k), element<DTYPE>(x[u], k + 1), nc2, scale2);
+            absorb_pair(s1, a1, element<DTYPE>(x[u], k + 2), element<DTYPE>(x[u], k + 3), nc2, scale2);
+        }
+    }
+    float p, q;
+    f2_unpack(f2_add(s0, s1), p, q);
+    t.s += p + q;
+    f2_unpack(f2_add(a0, a1), p, q);
+    t.a += p + q;
+}
+
+// the order of the alternatives: by logit, then by the lower id
+__device__ __forceinline__ bool before(float v, int i, float w, int j) { return v > w || (v == w && i < j); }
+
+// Sorted list of the best in a warp's lanes, lane 0 first; the same (v, i) in every lane goes in at its place.
+__device__ __forceinline__ void list_insert(float &lv, int &li, float v, int i, int lane)
+{
+    const int at = __popc(__ballot_sync(0xFFFFFFFFu, before(lv, li, v, i)));
+    const float uv = __shfl_up_sync(0xFFFFFFFFu, lv, 1);
+    const int ui = __shfl_up_sync(0xFFFFFFFFu, li, 1);
+    if (lane > at) { lv = uv; li = ui; }
+    if (lane == at) { lv = v; li = i; }
+}
+
+__device__ __forceinline__ void store_cluster(float *p, uint32_t rank, float v)
+{
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(od_cluster_address(p, rank)), "f"(v) : "memory");
+}
+__device__ __forceinline__ void store_cluster(int *p, uint32_t rank, int v)
+{
+    asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(od_cluster_address(p, rank)), "r"(v) : "memory");
+}
+
+// over a warp: the largest c, and the sums at it
+__device__ __forceinline__ Sums warp_total(Sums t, float scale)
+{
+    float g = t.c;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) g = fmaxf(g, __shfl_xor_sync(0xFFFFFFFFu, g, o));
+    t.raise(g, scale);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        t.s += __shfl_xor_sync(0xFFFFFFFFu, t.s, o);
+        t.a += __shfl_xor_sync(0xFFFFFFFFu, t.a, o);
+    }
+    return t;
+}
+
+// (a temperature whose reciprocal overflows is none)
+__device__ __forceinline__ bool usable(float T) { return T > 0.f && T < INFINITY && LOG2E / T < INFINITY; }
+
+template <int DTYPE, bool TOP>
+__global__ void __launch_bounds__(THREADS, 4) od_score_kernel(const ScoreArgs A)
+{
+    __shared__ float group_max[GROUPS];
+    __shared__ Sums warp_sums[WARPS], block_sums[MAX_SPLIT];
+    __shared__ float cand_v[TOP ? CAP : 1], list_v[TOP ? OD_MAX_TOP : 1], best_v[TOP ? MAX_SPLIT * OD_MAX_TOP : 1];
+    __shared__ int cand_i[TOP ? CAP : 1], list_i[TOP ? OD_MAX_TOP : 1], best_i[TOP ? MAX_SPLIT * OD_MAX_TOP : 1];
+    __shared__ int n_cand;
+
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t split = A.split, part = blockIdx.x % split;
+    const int64_t r = blockIdx.x / split;
+    const int32_t b = (int32_t)(r / A.R), rr = (int32_t)(r % A.R);
+    // (the blocks of a cluster leave together)
+    if (A.n_rows && rr >= A.n_rows[b]) return;
+    const float T = A.temperature ? A.temperature[b] : 1.f;
+    const char *row = A.logits + b * A.seq_bytes + rr * A.row_bytes;
+    const int V = A.V, n = A.n_top;
+    const int id = A.ids ? A.ids[r] : -1;
+    const uint32_t bad_id = id < -1 || id >= V ? OD_LF_BAD_ID : 0u;
+    if (!usable(T)) {
+        if (part == 0) {
+            if (tid == 0) {
+                A.row_max[r] = A.row_sum[r] = 0.f;
+                if (A.logprob) A.logprob[r] = 0.f;
+                if (A.entropy) A.entropy[r] = 0.f;
+                if (A.flags) A.flags[r] = OD_LF_BAD_TEMPERATURE | bad_id;
+            }
+            if (TOP && tid < n) { A.top_ids[r * n + tid] = -1; A.top_logprobs[r * n + tid] = -INFINITY; }
+        }
+        return;
+    }
+    od_cluster_arrive_relaxed();                           // waited for before this block writes into another
+    const float scale = LOG2E / T;
+    float x_t = 0.f;                                       // requested early, by the thread that uses it
+    if (tid == 0 && part == 0 && id >= 0 && id < V) x_t = od_load_logit<DTYPE>(row, id);
+
+    // the slice of this block, by vectors
+    const int nvec = (V - 1) / VEC<DTYPE> + 1;
+    const int lo = (int)((int64_t)nvec * part / split), hi = (int)((int64_t)nvec * (part + 1) / split);
+    const uint4 none = make_uint4(NONE<DTYPE>, NONE<DTYPE>, NONE<DTYPE>, NONE<DTYPE>);
+    Sums t = {-FLT_MAX, 0.f, 0.f};
+    {
+        uint4 x[U], y[U];
+        int i = lo + tid;
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = i + u * THREADS < hi ? load_vec<DTYPE>(row, i + u * THREADS, V) : none;
+        for (i += U * THREADS; i < hi; i += U * THREADS) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) y[u] = i + u * THREADS < hi ? load_vec<DTYPE>(row, i + u * THREADS, V) : none;
+            absorb<DTYPE>(t, x, scale);
+#pragma unroll
+            for (int u = 0; u < U; ++u) x[u] = y[u];
+        }
+        absorb<DTYPE>(t, x, scale);
+    }
+    if (TOP) {
+        float g = t.c;
+#pragma unroll
+        for (int o = 1; o < 8; o <<= 1) g = fmaxf(g, __shfl_xor_sync(0xFFFFFFFFu, g, o));
+        if ((lane & 7) == 0) group_max[tid >> 3] = g;
+        if (tid == 0) n_cand = 0;
+        if (tid < n) { list_v[tid] = -INFINITY; list_i[tid] = -1; }
+    }
+    const Sums w = warp_total(t, scale);
+    if (lane == 0) warp_sums[warp] = w;
+    __syncthreads();
+    if (TOP) {
+        // the bound: the largest logit of the group that has n - 1 others in front of it
+        const float g = group_max[lane];
+        int rank = 0;
+#pragma unroll
+        for (int k = 0; k < GROUPS; ++k) rank += before(group_max[k], k, g, lane);
+        const float bound = __shfl_sync(0xFFFFFFFFu, g, __ffs(__ballot_sync(0xFFFFFFFFu, rank == n - 1)) - 1);
+        for (unsigned left = __ballot_sync(0xFFFFFFFFu, t.c >= bound); left; left &= left - 1) {
+            // the elements of one thread, a vector to each lane
+            for (int i = lo + warp * 32 + __ffs(left) - 1 + lane * THREADS; i < hi; i += 32 * THREADS) {
+                const uint4 x = load_vec<DTYPE>(row, i, V);
+#pragma unroll
+                for (int k = 0; k < VEC<DTYPE>; ++k) {
+                    const float v = element<DTYPE>(x, k);
+                    if (v >= bound) {                      // (the bound is at least -FLT_MAX)
+                        const int at = atomicAdd(&n_cand, 1);
+                        if (at < CAP) { cand_v[at] = v; cand_i[at] = i * VEC<DTYPE> + k; }
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        int count = n_cand;
+        if (count > CAP) {
+            // many equal logits, or many of the largest in one thread: each warp lists the best of its elements
+            // instead, in the order of their ids, so that of equal ones the first n are all that goes in
+            __syncthreads();
+            float lv = -INFINITY;
+            int li = 0x7FFFFFFF;
+            for (int i0 = lo + warp * 32; i0 < hi; i0 += THREADS) {
+                const int i = i0 + lane;
+                const uint4 x = i < hi ? load_vec<DTYPE>(row, i, V) : none;
+                const float last_v = __shfl_sync(0xFFFFFFFFu, lv, n - 1);
+                const int last_i = __shfl_sync(0xFFFFFFFFu, li, n - 1);
+#pragma unroll
+                for (int k = 0; k < VEC<DTYPE>; ++k) {
+                    const float v = element<DTYPE>(x, k);
+                    unsigned in = __ballot_sync(0xFFFFFFFFu, v >= bound && before(v, i * VEC<DTYPE> + k, last_v, last_i));
+                    for (; in; in &= in - 1) {
+                        const int from = __ffs(in) - 1;
+                        list_insert(lv, li, __shfl_sync(0xFFFFFFFFu, v, from), (i0 + from) * VEC<DTYPE> + k, lane);
+                    }
+                }
+            }
+            if (lane < n) { cand_v[warp * n + lane] = lv; cand_i[warp * n + lane] = li; }
+            __syncthreads();
+            count = WARPS * n;
+        }
+        for (int j = tid; j < count; j += THREADS) {       // rank by counting
+            const float v = cand_v[j];
+            const int i = cand_i[j];
+            int rank = 0;
+            for (int k = 0; k < count; ++k) rank += before(cand_v[k], cand_i[k], v, i);
+            if (v > -INFINITY && rank < n) { list_v[rank] = v; list_i[rank] = i; }
+        }
+        __syncthreads();
+    }
+    // the parts of the row to its cluster's first block
+    Sums all = {-FLT_MAX, 0.f, 0.f};
+    if (lane < WARPS) all = warp_sums[lane];
+    all = warp_total(all, scale);
+    od_cluster_wait();
+    if (TOP && tid < n) {
+        store_cluster(best_v + part * n + tid, 0, list_v[tid]);
+        store_cluster(best_i + part * n + tid, 0, list_i[tid]);
+    }
+    if (tid < 3) store_cluster((float *)(block_sums + part) + tid, 0, tid == 0 ? all.c : tid == 1 ? all.s : all.a);
+    od_cluster_arrive();
+    if (part != 0) return;                                 // (nobody writes into this block)
+    od_cluster_wait();
+    all = {-FLT_MAX, 0.f, 0.f};
+    if (lane < (int)split) all = block_sums[lane];
+    all = warp_total(all, scale);
+    const bool finite = all.s == all.s, empty = all.s == 0.f;
+    const float nan = __int_as_float(0x7FFFFFFF), ln_s = logf(all.s);
+    if (tid == 0) {
+        A.row_max[r] = !finite ? nan : empty ? -INFINITY : all.c;
+        A.row_sum[r] = all.s;
+        float lp = 0.f;
+        if (id >= 0 && id < V) lp = empty ? -INFINITY : (x_t - all.c) / T - ln_s;
+        if (id >= 0 && id < V && !finite) lp = nan;
+        if (A.logprob) A.logprob[r] = lp;
+        if (A.entropy) A.entropy[r] = empty ? 0.f : ln_s - LN2 * (all.a / all.s);
+        if (A.flags) A.flags[r] = (finite ? 0u : OD_LF_NONFINITE) | (empty ? OD_LF_NO_MASS : 0u) | bad_id;
+    }
+    if (TOP) {
+        const int count = (int)split * n;
+        if (!finite) {
+            if (tid < n) { A.top_ids[r * n + tid] = -1; A.top_logprobs[r * n + tid] = nan; }
+            return;
+        }
+        int filled = 0;                                    // alternatives that there are
+        for (int k = 0; k < count; ++k) filled += best_i[k] >= 0;
+        for (int j = tid; j < count; j += THREADS) {
+            const float v = best_v[j];
+            const int i = best_i[j];
+            if (i < 0) continue;
+            int rank = 0;
+            for (int k = 0; k < count; ++k) rank += best_i[k] >= 0 && before(best_v[k], best_i[k], v, i);
+            if (rank < n) {
+                A.top_ids[r * n + rank] = i;
+                A.top_logprobs[r * n + rank] = (v - all.c) / T - ln_s;
+            }
+        }
+        if (tid < n && tid >= filled) { A.top_ids[r * n + tid] = -1; A.top_logprobs[r * n + tid] = -INFINITY; }
+    }
+}
+
+// ---- the gradient ------------------------------------------------------------------------------
+
+struct ScoreGradArgs {
+    const char *logits;
+    int64_t row_bytes, seq_bytes;
+    char *grad;
+    int64_t grad_row_bytes, grad_seq_bytes;
+    int32_t R, V, n_top, chunks;                           // blocks of a row
+    const int32_t *ids, *n_rows, *top_ids;
+    const float *temperature, *row_max, *row_sum, *entropy, *g_logprob, *g_entropy, *g_top;
+};
+
+constexpr int CHUNK = U * THREADS;                         // vectors of a block
+
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi)
+{
+    uint32_t d;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+template <int DTYPE>
+__device__ __forceinline__ void store_element(char *row, int j, float v)
+{
+    if (DTYPE == OD_F32) ((float *)row)[j] = v;
+    else ((unsigned short *)row)[j] = (unsigned short)bf16x2(v, 0.f);
+}
+template <int DTYPE>
+__device__ __forceinline__ void store_vec(char *row, int i, int V, const float (&v)[VEC<DTYPE>])
+{
+    if (i < V / VEC<DTYPE>) {
+        uint4 o;
+        if constexpr (DTYPE == OD_F32)
+            o = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        else
+            o = make_uint4(bf16x2(v[0], v[1]), bf16x2(v[2], v[3]), bf16x2(v[4], v[5]), bf16x2(v[6], v[7]));
+        *(uint4 *)(row + (size_t)i * 16) = o;
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < VEC<DTYPE>; ++k)
+        if (i * VEC<DTYPE> + k < V) store_element<DTYPE>(row, i * VEC<DTYPE> + k, v[k]);
+}
+
+// grad may be the logits themselves: an element is written by the thread that has read it, the given ones behind a
+// barrier from logits that were read in front of it.
+template <int DTYPE>
+__global__ void __launch_bounds__(THREADS) od_score_grad_kernel(const ScoreGradArgs A)
+{
+    constexpr int GIVEN = OD_MAX_TOP + 1;
+    __shared__ int given_id[GIVEN];
+    __shared__ float given_g[GIVEN];
+
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int64_t r = blockIdx.x / A.chunks;
+    const int chunk = blockIdx.x % A.chunks, V = A.V, n = A.n_top;
+    const int32_t b = (int32_t)(r / A.R), rr = (int32_t)(r % A.R);
+    const char *row = A.logits + b * A.seq_bytes + rr * A.row_bytes;
+    char *out = A.grad + b * A.grad_seq_bytes + rr * A.grad_row_bytes;
+    const int nvec = (V - 1) / VEC<DTYPE> + 1, lo = chunk * CHUNK, hi = min(nvec, lo + CHUNK);
+    const bool counts = !A.n_rows || rr < A.n_rows[b];
+    const float T = A.temperature ? A.temperature[b] : 1.f;
+    const float S = counts ? A.row_sum[r] : 0.f;
+    if (!counts || !usable(T) || S == 0.f) {
+        const float zero[VEC<DTYPE>] = {};
+        for (int i = lo + tid; i < hi; i += THREADS) store_vec<DTYPE>(out, i, V, zero);
+        return;
+    }
+    uint4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (lo + u * THREADS + tid < hi) x[u] = load_vec<DTYPE, false>(row, lo + u * THREADS + tid, V);
+
+    // every warp sums the weights itself, in the same order
+    const float M = A.row_max[r], ln_s = logf(S), scale = LOG2E / T;
+    const int id = A.ids && A.g_logprob ? A.ids[r] : -1;
+    const bool given = id >= 0 && id < V;
+    const float g_id = given ? A.g_logprob[r] : 0.f;
+    int top = -1;
+    float g = 0.f;
+    if (A.g_top && lane < n) top = A.top_ids[r * n + lane];
+    if (top >= V) top = -1;
+    if (top >= 0) g = A.g_top[r * n + lane];
+    float G = g;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) G += __shfl_xor_sync(0xFFFFFFFFu, G, o);
+    G += g_id;
+    if (tid < 32) { given_id[lane] = top; given_g[lane] = g; }
+    if (tid == 0) { given_id[OD_MAX_TOP] = given ? id : -1; given_g[OD_MAX_TOP] = g_id; }
+    __syncthreads();
+    const float g_h = A.g_entropy ? A.g_entropy[r] : 0.f, per = -1.f / (S * T);
+    const float c0 = per * (G + (A.g_entropy ? g_h * (A.entropy[r] - ln_s) : 0.f)), c1 = per * g_h * LN2;
+
+    // the value of a given id in this chunk: it is written by the first entry that names it, with the sum of their weights
+    int write = -1;
+    float value = 0.f;
+    if (tid < GIVEN) {
+        const int j = given_id[tid], i = j / VEC<DTYPE>;
+        if (j >= 0 && i >= lo && i < hi) {
+            float sum = 0.f;
+            bool first = true;
+            for (int k = 0; k < GIVEN; ++k)
+                if (given_id[k] == j) { sum += given_g[k]; first = first && k >= tid; }
+            if (first) {
+                const float xj = DTYPE == OD_F32 ? __ldcs((const float *)row + j) : __uint_as_float((uint32_t)__ldcs((const unsigned short *)row + j) << 16);
+                const float d = (xj - M) * scale;
+                value = od_ex2(d) * (c0 + c1 * fmaxf(d, LEAST)) + sum / T;
+                write = j;
+            }
+        }
+    }
+    // (in front of every store: they may be to the logits that were read above)
+    __syncthreads();
+    const uint64_t nm2 = f2_pack(-M, -M), scale2 = f2_pack(scale, scale), c02 = f2_pack(c0, c0), c12 = f2_pack(c1, c1);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int i = lo + u * THREADS + tid;
+        if (i >= hi) break;
+        float v[VEC<DTYPE>];
+#pragma unroll
+        for (int k = 0; k < VEC<DTYPE>; k += 2) {
+            float d0, d1;
+            f2_unpack(f2_mul(f2_add(f2_pack(element<DTYPE>(x[u], k), element<DTYPE>(x[u], k + 1)), nm2), scale2), d0, d1);
+            const uint64_t e2 = f2_pack(od_ex2(d0), od_ex2(d1));
+            f2_unpack(f2_mul(e2, f2_fma(f2_pack(fmaxf(d0, LEAST), fmaxf(d1, LEAST)), c12, c02)), v[k], v[k + 1]);
+        }
+        store_vec<DTYPE>(out, i, V, v);
+    }
+    __syncthreads();
+    if (write >= 0) store_element<DTYPE>(out, write, value);
+}
+
+template <typename K, typename A>
+cudaError_t launch(K kernel, unsigned blocks, unsigned cluster, bool pdl, const A &args, cudaStream_t s)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(blocks); cfg.blockDim = dim3(THREADS);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = pdl ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args);
+}
+
+}  // namespace
+
+cudaError_t od_launch_score(const od_ctx *c, int32_t B, int32_t R, int32_t V, const void *logits, int32_t dtype, int64_t row_stride,
+                            int64_t seq_stride, const int32_t *ids, const int32_t *n_rows, const float *temperature, int32_t n_top,
+                            float *logprob, float *entropy, float *row_max, float *row_sum, int32_t *top_ids, float *top_logprobs,
+                            uint32_t *flags, cudaStream_t s)
+{
+    const int64_t esz = dtype == OD_BF16 ? 2 : 4, rows = (int64_t)B * R;
+    // Blocks of a row: as many as give every multiprocessor two, while a block's slice stays 8 KB or more.
+    int32_t split = 1;
+    while (split < MAX_SPLIT && rows * split < 2 * c->sm_count && (int64_t)V * esz / split >= 16384) split *= 2;
+    const ScoreArgs a = {(const char *)logits, row_stride * esz, seq_stride * esz, R, V, n_top, split, ids, n_rows, temperature,
+                         logprob, entropy, row_max, row_sum, top_logprobs, top_ids, flags};
+    const unsigned blocks = (unsigned)(rows * split);
+    const bool pdl = c->opt_pdl != 0;
+    if (dtype == OD_BF16)
+        return n_top ? launch(od_score_kernel<OD_BF16, true>, blocks, split, pdl, a, s) : launch(od_score_kernel<OD_BF16, false>, blocks, split, pdl, a, s);
+    return n_top ? launch(od_score_kernel<OD_F32, true>, blocks, split, pdl, a, s) : launch(od_score_kernel<OD_F32, false>, blocks, split, pdl, a, s);
+}
+
+int64_t od_score_grad_blocks(int64_t rows, int32_t V, int32_t dtype)
+{
+    const int32_t nvec = dtype == OD_BF16 ? (V - 1) / VEC<OD_BF16> + 1 : (V - 1) / VEC<OD_F32> + 1;
+    return rows * ((nvec + CHUNK - 1) / CHUNK);
+}
+
+cudaError_t od_launch_score_grad(const od_ctx *c, int32_t B, int32_t R, int32_t V, const void *logits, int32_t dtype, int64_t row_stride,
+                                 int64_t seq_stride, const int32_t *ids, const int32_t *n_rows, const float *temperature,
+                                 const float *row_max, const float *row_sum, const float *entropy, int32_t n_top,
+                                 const int32_t *top_ids, const float *g_logprob, const float *g_entropy, const float *g_top, void *grad,
+                                 int64_t grad_row_stride, int64_t grad_seq_stride, cudaStream_t s)
+{
+    const int64_t esz = dtype == OD_BF16 ? 2 : 4, blocks = od_score_grad_blocks((int64_t)B * R, V, dtype);
+    const ScoreGradArgs a = {(const char *)logits, row_stride * esz, seq_stride * esz, (char *)grad, grad_row_stride * esz,
+                             grad_seq_stride * esz, R, V, n_top, (int32_t)(blocks / ((int64_t)B * R)), ids, n_rows, top_ids, temperature,
+                             row_max, row_sum, entropy, g_logprob, g_entropy, g_top};
+    return dtype == OD_BF16 ? launch(od_score_grad_kernel<OD_BF16>, (unsigned)blocks, 1, c->opt_pdl != 0, a, s)
+                            : launch(od_score_grad_kernel<OD_F32>, (unsigned)blocks, 1, c->opt_pdl != 0, a, s);
+}
