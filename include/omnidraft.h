@@ -449,6 +449,36 @@ int32_t od_token_logprobs_grad(od_ctx *ctx, int32_t B, int32_t R, int32_t vocab,
                                const float *g_entropy, const float *g_top, void *grad,
                                int64_t grad_row_stride, int64_t grad_seq_stride, void *stream);
 
+/* ---- an output layer with 4-bit weights ------------------------------------ */
+
+/* The logits of a few tokens from an output layer (the drafter's, on a device that holds it in 4
+ * bits) and the way of a gradient with respect to them (od_distill_loss's, od_token_logprobs_grad's) back
+ * to the hidden states:
+ *   w[v,h] = scales[v, h / group] * (code[v,h] - 8),
+ *   logits[n,v] = sum_h hidden[n,h] w[v,h],   g_hidden[n,h] = sum_v g_logits[n,v] w[v,h].
+ * Sums are fp32, nothing is rounded before them: a product of an input and a code is exact, scales
+ * are applied to sums over a group (logits; such a sum has to stay within fp32's range) or to the
+ * input (gradient, one fp32 rounding).
+ *   in  (device) hidden / g_logits fp32 or bf16, N rows, row stride in elements, base and stride
+ *                multiples of 16 bytes
+ *                codes  uint8[vocab, hidden_size / 2], dense, 16-byte aligned: column 2i of a row in
+ *                       the low half of its byte i, column 2i + 1 in the high half
+ *                scales bf16[vocab, hidden_size / group], dense; group = 32, 64 or 128 (UNSUPPORTED
+ *                       otherwise) and hidden_size a multiple of it, at most 65536
+ *   out (device) logits / g_hidden fp32 or bf16, N rows, base and stride multiples of 16 bytes;
+ *                nothing behind a row is written
+ * Neither vocab nor N is bound to the context. Made for N up to some dozens of tokens: the weights are
+ * unpacked again for every few of them. Asynchronous on `stream`; no scratch, the same results in
+ * every run. */
+int32_t od_q4_logits(od_ctx *ctx, int32_t N, int32_t vocab, int32_t hidden_size, int32_t group,
+                     const void *hidden, int32_t hidden_dtype, int64_t hidden_stride,
+                     const void *codes, const void *scales, void *logits, int32_t logit_dtype,
+                     int64_t logit_stride, void *stream);
+int32_t od_q4_logits_grad(od_ctx *ctx, int32_t N, int32_t vocab, int32_t hidden_size, int32_t group,
+                          const void *g_logits, int32_t logit_dtype, int64_t logit_stride,
+                          const void *codes, const void *scales, void *g_hidden,
+                          int32_t hidden_dtype, int64_t hidden_stride, void *stream);
+
 /* Adaptive drafting, exit rule (Section 3.3, Eq. (4)-(6)). From the acceptance
  * head's outputs f_phi(e_i) of the proposed tokens:
  *   reject_prob[b,k] = 1 - prod_{i<=k} sigmoid(head_logits[b,i])   (some token up

@@ -26,7 +26,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libomnidraft.so")
 
 OD_F32, OD_BF16 = 0, 1
-OD_ERR_INVALID_ARG, OD_ERR_ALIGNMENT = -1, -2
+OD_ERR_INVALID_ARG, OD_ERR_ALIGNMENT, OD_ERR_UNSUPPORTED = -1, -2, -5
 OD_TAIL_COMPLETE, OD_TAIL_UNMAPPED_STOP = 0, 1
 OD_CNT_CACHE_HITS, OD_CNT_UNMAPPED_STOPS, OD_CNT_INVALID_IDS, OD_CNT_MAPPED_TOKENS = 0, 1, 2, 3
 OD_CNT_COUNT = 4
@@ -42,7 +42,7 @@ EXPORTS = ["od_create", "od_destroy", "od_set_vocab_map", "od_cache_build", "od_
            "od_map_proposals", "od_verify", "od_sample_residual", "od_step", "od_host_step_reserve",
            "od_step_host", "od_verify_noalloc", "od_exit_rule", "od_cache_configure", "od_cache_set_clock",
            "od_cache_insert", "od_cache_trim", "od_cache_dump", "od_cache_stats", "od_distill_loss",
-           "od_token_logprobs", "od_token_logprobs_grad",
+           "od_token_logprobs", "od_token_logprobs_grad", "od_q4_logits", "od_q4_logits_grad",
            "od_verify_shard_stats", "od_verify_shard_finish", "od_sample_shard_mass", "od_sample_shard_pick",
            "od_last_launch_info", "od_status_string", "od_version"]
 
@@ -85,6 +85,8 @@ def lib():
         L.od_token_logprobs.argtypes = [vp, i32, i32, i32, vp, i32, i64, i64, vp, vp, vp, i32] + [vp] * 7 + [vp]
         L.od_token_logprobs_grad.argtypes = ([vp, i32, i32, i32, vp, i32, i64, i64] + [vp] * 6 + [i32] + [vp] * 5
                                              + [i64, i64, vp])
+        for name in ("od_q4_logits", "od_q4_logits_grad"):
+            getattr(L, name).argtypes = [vp, i32, i32, i32, i32, vp, i32, i64, vp, vp, vp, i32, i64, vp]
         L.od_verify_shard_stats.argtypes = [vp, i32, i32, i32, i32, vp, i32, i64, i64] + [vp] * 4 + [vp]
         L.od_verify_shard_finish.argtypes = [vp, i32, i32, i32] + [vp] * 7 + [u64] + [vp] * 7 + [vp]
         L.od_sample_shard_mass.argtypes = [vp, i32, i32, i32, i32, vp, i32, i64, i64] + [vp] * 12 + [vp] + [vp]
@@ -489,6 +491,54 @@ def od_token_logprobs_grad(ctx: Context, logits, ids, lp: LogprobOut, g_logprob=
         _dp(g_entropy, f32, d), _dp(g_top, f32, d), C.c_void_p(grad.data_ptr()), grs, gss, _stream(d)),
         "od_token_logprobs_grad")
     return grad
+
+
+# ---- an output layer with 4-bit weights, and its gradient ----
+
+def _flat_rows(t: torch.Tensor, width: int, device, what: str):
+    """(rows, row stride) of [..., width] whose rows are all equally far apart."""
+    if t.dim() not in (2, 3) or t.shape[-1] != width:
+        raise ValueError(f"{what} must be [N, {width}] or [B, K, {width}], got {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{what} on another device")
+    if t.numel() == 0:
+        return 0, width
+    _, R, V, row, seq = _row_strides(t if t.dim() == 3 else t[None], device, what)
+    if t.dim() == 3 and seq != row * R:
+        raise ValueError(f"the rows of {what} must be equally far apart")
+    return t.numel() // V, row
+
+
+def _q4(ctx: Context, x, codes, scales, out, dtype, backward: bool):
+    d = ctx.device
+    V, H = int(codes.shape[0]), int(codes.shape[1]) * 2
+    if codes.dim() != 2 or scales.dim() != 2 or scales.shape[0] != V or scales.shape[1] < 1 or H % scales.shape[1]:
+        raise ValueError("codes must be [V, H / 2] and scales [V, H / group]")
+    wide, wide_out = (V, H) if backward else (H, V)
+    if out is None:
+        per = 4 if dtype == torch.float32 else 8
+        out = torch.empty(*x.shape[:-1], -(-wide_out // per) * per, dtype=dtype, device=d)[..., :wide_out]
+    if out.shape[:-1] != x.shape[:-1]:
+        raise ValueError("the rows of out must be those of the input")
+    n, xs = _flat_rows(x, wide, d, "g_logits" if backward else "hidden")
+    _, ys = _flat_rows(out, wide_out, d, "out")
+    name = "od_q4_logits_grad" if backward else "od_q4_logits"
+    _check(getattr(lib(), name)(
+        ctx.handle, n, V, H, H // int(scales.shape[1]), C.c_void_p(x.data_ptr()), logit_dtype_code(x), xs,
+        _dp(codes, torch.uint8, d), _dp(scales, torch.bfloat16, d), C.c_void_p(out.data_ptr()), logit_dtype_code(out),
+        ys, _stream(d)), name)
+    return out
+
+
+def od_q4_logits(ctx: Context, hidden, codes, scales, out=None, dtype=torch.float32):
+    """Logits [..., V] (rows padded to 16 bytes) of hidden states [..., H], from codes uint8 [V, H / 2] and scales
+    bf16 [V, H / group]."""
+    return _q4(ctx, hidden, codes, scales, out, dtype, False)
+
+
+def od_q4_logits_grad(ctx: Context, g_logits, codes, scales, out=None, dtype=torch.float32):
+    """The gradient [..., H] with respect to the hidden states from that of the logits, [..., V]."""
+    return _q4(ctx, g_logits, codes, scales, out, dtype, True)
 
 
 def od_exit_rule(ctx: Context, head_logits, avail_len, gamma: float):

@@ -99,6 +99,15 @@ int32_t check_row_tensor(int32_t vocab, const void *rows, int32_t dtype, int32_t
     return check_logits_len(vocab, rows, dtype, row_stride, seq_stride, R - 1);
 }
 
+// a layer of 4-bit weights
+int32_t check_q4(const od_ctx *c, int32_t N, int32_t vocab, int32_t hidden_size, int32_t group, const void *codes, const void *scales)
+{
+    if (!c || N < 0 || vocab < 1 || hidden_size < 1 || !codes || !scales) return OD_ERR_INVALID_ARG;
+    if ((group != 32 && group != 64 && group != 128) || hidden_size > 65536 || vocab > (1 << 30) || N > 65535) return OD_ERR_UNSUPPORTED;
+    if (hidden_size % group != 0) return OD_ERR_INVALID_ARG;
+    return aligned16(codes) && ((uintptr_t)scales & 1u) == 0 ? OD_OK : OD_ERR_ALIGNMENT;
+}
+
 // a vocabulary shard: whole 256-id tiles, inside the vocabulary
 int32_t check_shard(const od_ctx *c, int32_t shard_lo, int32_t shard_len)
 {
@@ -684,6 +693,38 @@ int32_t od_token_logprobs_grad(od_ctx *c, int32_t B, int32_t R, int32_t vocab, c
     OD_CUDA(od_launch_score_grad(c, B, R, vocab, logits, logit_dtype, row_stride, seq_stride, ids, n_rows, temperature, row_max,
                                  row_sum, entropy, n_top, top_ids, g_logprob, g_entropy, g_top, grad, grad_row_stride,
                                  grad_seq_stride, (cudaStream_t)stream));
+    return OD_OK;
+}
+
+int32_t od_q4_logits(od_ctx *c, int32_t N, int32_t vocab, int32_t hidden_size, int32_t group, const void *hidden,
+                     int32_t hidden_dtype, int64_t hidden_stride, const void *codes, const void *scales, void *logits,
+                     int32_t logit_dtype, int64_t logit_stride, void *stream)
+{
+    int32_t st = check_q4(c, N, vocab, hidden_size, group, codes, scales);
+    if (st != OD_OK || N == 0) return st;
+    st = check_logits_len(hidden_size, hidden, hidden_dtype, hidden_stride, hidden_stride, 0);
+    if (st == OD_OK) st = check_logits_len(vocab, logits, logit_dtype, logit_stride, logit_stride, 0);
+    if (st != OD_OK) return st;
+    DeviceGuard g(c->device);
+    if (!g.ok) return OD_ERR_CUDA;
+    OD_CUDA(od_launch_q4(c, false, N, vocab, hidden_size, group, hidden, hidden_dtype, hidden_stride, codes, scales, logits,
+                         logit_dtype, logit_stride, (cudaStream_t)stream));
+    return OD_OK;
+}
+
+int32_t od_q4_logits_grad(od_ctx *c, int32_t N, int32_t vocab, int32_t hidden_size, int32_t group, const void *g_logits,
+                          int32_t logit_dtype, int64_t logit_stride, const void *codes, const void *scales, void *g_hidden,
+                          int32_t hidden_dtype, int64_t hidden_stride, void *stream)
+{
+    int32_t st = check_q4(c, N, vocab, hidden_size, group, codes, scales);
+    if (st != OD_OK || N == 0) return st;
+    st = check_logits_len(vocab, g_logits, logit_dtype, logit_stride, logit_stride, 0);
+    if (st == OD_OK) st = check_logits_len(hidden_size, g_hidden, hidden_dtype, hidden_stride, hidden_stride, 0);
+    if (st != OD_OK) return st;
+    DeviceGuard g(c->device);
+    if (!g.ok) return OD_ERR_CUDA;
+    OD_CUDA(od_launch_q4(c, true, N, vocab, hidden_size, group, g_logits, logit_dtype, logit_stride, codes, scales, g_hidden,
+                         hidden_dtype, hidden_stride, (cudaStream_t)stream));
     return OD_OK;
 }
 

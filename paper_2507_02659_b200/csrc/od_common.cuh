@@ -316,6 +316,10 @@ cudaError_t od_launch_score_grad(const od_ctx *c, int32_t B, int32_t R, int32_t 
                                  const int32_t *top_ids, const float *g_logprob, const float *g_entropy, const float *g_top, void *grad,
                                  int64_t grad_row_stride, int64_t grad_seq_stride, cudaStream_t s);
 
+// an output layer with 4-bit weights: logits b of hidden states a, or (backward) their gradient b of the logits' a
+cudaError_t od_launch_q4(const od_ctx *c, bool backward, int32_t N, int32_t V, int32_t H, int32_t G, const void *a, int32_t a_dtype,
+                         int64_t as, const void *codes, const void *scales, void *b, int32_t b_dtype, int64_t bs, cudaStream_t s);
+
 void od_cache_free_dynamic(od_ctx *c);   // frees what od_cache_configure allocated beyond keys / vals
 
 cudaError_t od_launch_exit(int32_t B, int32_t K_max, const float *head_logits, const int32_t *avail_len,

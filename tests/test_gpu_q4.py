@@ -1,0 +1,276 @@
+"""od_q4_logits and od_q4_logits_grad against products in 64 bits.
+
+Tolerances. A product of an input and a code is exact (an fp32 input is taken in three bf16 pieces, a scaled bf16 one in
+two), so the errors are those of fp32 sums: a matrix instruction adds sixteen products to its accumulator with an
+error of at most 2^-22 of the largest sum of magnitudes it meets, an fp32 step 2^-24. With S = sum |x w| a logit
+goes through group / 16 * 3 instructions per group and one step per group; a gradient through at most
+vocab / 16 * 3 instructions, one rounding of each scaled input, and the steps that join the parts (below 64).
+The result is rounded once to its type.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2507_02659_b200 import binding as od
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+HALF = {BF16: 2.0 ** -8, F32: 2.0 ** -24}
+
+
+@pytest.fixture(scope="module")
+def ctx(cuda_device):
+    torch.cuda.set_device(cuda_device)
+    c = od.Context(cuda_device, 10, 10, 1, 1)
+    yield c
+    c.close()
+
+
+def padded(x, fill=float("nan")):
+    """The same rows, 16-byte strides; what lies behind a row is NaN."""
+    per = 16 // x.element_size()
+    store = torch.full((*x.shape[:-1], (x.shape[-1] // per + 2) * per), fill, dtype=x.dtype, device=x.device)
+    store[..., :x.shape[-1]] = x
+    return store[..., :x.shape[-1]]
+
+
+def layer(V, H, G, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    codes = torch.randint(0, 256, (V, H // 2), generator=g, device="cuda", dtype=torch.uint8)
+    scales = (torch.rand(V, H // G, generator=g, device="cuda") + 0.1) * torch.where(torch.rand(V, H // G, generator=g, device="cuda") < 0.1, -1, 1)
+    return codes, scales.to(BF16)
+
+
+def weights(codes, scales):
+    V, H = codes.shape[0], codes.shape[1] * 2
+    w = torch.empty(V, H, dtype=torch.float64, device="cuda")
+    w[:, 0::2], w[:, 1::2] = (codes % 16).double() - 8, (codes // 16).double() - 8
+    return w * scales.double().repeat_interleave(H // scales.shape[1], 1)
+
+
+def same(got, want, tol):
+    got = got.double()
+    tol = tol + HALF[F32] * want.abs()
+    bad = ~((got - want).abs() <= tol)
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()}: {got[bad][:4].tolist()} for {want[bad][:4].tolist()}, tolerance {tol[bad][:4].tolist()}"
+
+
+def check_logits(got, x, w, G):
+    want, size = x.double() @ w.T, x.double().abs() @ w.abs().T
+    tol = size * (G / 16 * 3 * 2.0 ** -22 + (w.shape[1] / G + 4) * 2.0 ** -24)
+    same(got, want, tol + HALF[got.dtype] * (want.abs() + tol))
+
+
+def check_grad(got, dy, w):
+    want, size = dy.double() @ w, dy.double().abs() @ w.abs()
+    tol = size * (math.ceil(w.shape[0] / 16) * 3 * 2.0 ** -22 + 64 * 2.0 ** -24)
+    same(got, want, tol + HALF[got.dtype] * (want.abs() + tol))
+
+
+# tokens, vocabulary, hidden size, group
+SIZES = [(1, 1, 32, 32), (2, 3, 64, 64), (1, 16, 128, 128), (7, 17, 96, 32), (8, 31, 1056, 32), (9, 100, 320, 64), (1, 1000, 768, 128),
+         (16, 515, 4096, 128), (17, 2000, 1152, 64), (33, 333, 640, 32), (64, 1025, 512, 128), (5, 4099, 2048, 64), (3, 40, 16384, 128),
+         (1, 9, 65536, 64), (12, 20011, 256, 32)]
+TYPES = [(BF16, F32), (BF16, BF16), (F32, F32), (F32, BF16)]
+
+
+@pytest.mark.parametrize("given,made", TYPES)
+@pytest.mark.parametrize("N,V,H,G", SIZES)
+def test_logits(ctx, N, V, H, G, given, made):
+    codes, scales = layer(V, H, G, 1)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = padded(torch.randn(N, H, generator=g, device="cuda").to(given))
+    per = 16 // torch.empty(0, dtype=made).element_size()
+    store = torch.full((N + 1, (V // per + 2) * per), 55.0, dtype=made, device="cuda")
+    out = od.od_q4_logits(ctx, x, codes, scales, out=store[:N, :V])
+    check_logits(out, x, weights(codes, scales), G)
+    assert (store[N] == 55).all() and (store[:, V:] == 55).all()
+    assert torch.equal(out, od.od_q4_logits(ctx, x, codes, scales, dtype=made))      # the same in every run
+
+
+@pytest.mark.parametrize("given,made", TYPES)
+@pytest.mark.parametrize("N,V,H,G", SIZES)
+def test_gradient(ctx, N, V, H, G, given, made):
+    codes, scales = layer(V, H, G, 3)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    dy = padded(torch.randn(N, V, generator=g, device="cuda").to(given))
+    store = torch.full((N + 1, H + 32), 55.0, dtype=made, device="cuda")
+    out = od.od_q4_logits_grad(ctx, dy, codes, scales, out=store[:N, :H])
+    check_grad(out, dy, weights(codes, scales))
+    assert (store[N] == 55).all() and (store[:, H:] == 55).all()
+    assert torch.equal(out, od.od_q4_logits_grad(ctx, dy, codes, scales, dtype=made))
+
+
+def test_every_code_and_column(ctx):
+    """Unit vectors read single weights: every code at every place of a word, each group's own scale."""
+    V, H, G = 16, 256, 64
+    u = (torch.arange(V, device="cuda")[:, None] + 5 * torch.arange(H, device="cuda")[None]) % 16
+    codes = (u[:, 0::2] | u[:, 1::2] << 4).to(torch.uint8)
+    scales = (2.0 ** (torch.arange(V, device="cuda")[:, None] - 2.0 * torch.arange(H // G, device="cuda")[None])).to(BF16)
+    w = weights(codes, scales)
+    for dtype in (BF16, F32):
+        assert torch.equal(od.od_q4_logits(ctx, torch.eye(H, device="cuda").to(dtype), codes, scales).double(), w.T)
+        assert torch.equal(od.od_q4_logits_grad(ctx, torch.eye(V, device="cuda").to(dtype), codes, scales).double(), w)
+
+
+def test_fp32_inputs_keep_their_digits(ctx):
+    """Inputs that differ in their last bits only: what is left of them after they cancel is exact."""
+    V, H, G = 40, 64, 32
+    codes = torch.full((V, H // 2), 0x97, dtype=torch.uint8, device="cuda")          # -1 in even columns, +1 in odd ones
+    scales = torch.ones(V, H // G, dtype=BF16, device="cuda")
+    x = torch.zeros(1, H, device="cuda")
+    x[0, 6], x[0, 7] = 1.0 + 2.0 ** -23, 1.0 + 3 * 2.0 ** -23
+    assert (od.od_q4_logits(ctx, x, codes, scales) == 2.0 ** -22).all()
+    codes[0::2] = 0x79
+    dy = padded(torch.zeros(1, V, device="cuda"))
+    dy[0, 4], dy[0, 5] = 1.0 + 2.0 ** -23, 1.0 + 3 * 2.0 ** -23
+    got = od.od_q4_logits_grad(ctx, dy, codes, scales)
+    assert (got[0, 0::2] == -2.0 ** -22).all() and (got[0, 1::2] == 2.0 ** -22).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_inputs_at_the_limits(ctx, dtype):
+    """Infinities and NaN reach the results that the formula has them in, and no others; the largest and smallest finite values stay finite."""
+    N, V, H, G = 9, 50, 128, 32
+    codes, scales = layer(V, H, G, 5)
+    codes[:, 3] = 0x99                                      # columns 6 and 7: +1 everywhere
+    w = weights(codes, scales)
+    x = torch.randn(N, H, device="cuda").to(dtype)
+    x[1, 6], x[2, 6], x[3, 6] = math.inf, -math.inf, float("nan")
+    y = od.od_q4_logits(ctx, x, codes, scales)
+    sign = torch.sign(w[:, 6])
+    assert torch.equal(y[1], (sign * math.inf).float()) and torch.equal(y[2], (-sign * math.inf).float()) and torch.isnan(y[3]).all()
+    keep = [0, 4, 5, 6, 7, 8]
+    check_logits(y[keep], x[keep], w, G)
+    dy = padded(torch.randn(N, V, device="cuda").to(dtype))
+    codes[4] = 0x99
+    w = weights(codes, scales)
+    dy[1, 4], dy[2, 4] = math.inf, float("nan")
+    dx = od.od_q4_logits_grad(ctx, dy, codes, scales)
+    assert torch.equal(dx[1], (torch.sign(w[4]) * math.inf).float()) and torch.isnan(dx[2]).all()
+    keep = [0] + list(range(3, N))
+    check_grad(dx[keep], dy[keep], w)
+    # the type's largest value, and tiny ones, through weights of a half
+    codes.fill_(0x88); codes[:, 0] = 0x89; scales.fill_(0.5)
+    x = torch.zeros(2, H, device="cuda", dtype=dtype)
+    x[0, 0], x[1, 0] = torch.finfo(dtype).max, 2.0 ** -126
+    assert torch.equal(od.od_q4_logits(ctx, x, codes, scales), (x[:, :1].double() / 2).float().expand(2, V))
+    dy = padded(torch.zeros(2, V, device="cuda", dtype=dtype))
+    dy[0, 3], dy[1, 3] = torch.finfo(dtype).max, 2.0 ** -110
+    assert torch.equal(od.od_q4_logits_grad(ctx, dy, codes, scales)[:, 0], (dy[:, 3].double() / 2).float())
+
+
+def test_the_gradient_is_the_transpose(ctx):
+    """<y, dy> = <x, dx>: the two products use the same weights."""
+    N, V, H, G = 6, 700, 384, 64
+    codes, scales = layer(V, H, G, 6)
+    x, dy = torch.randn(N, H, device="cuda"), padded(torch.randn(N, V, device="cuda"))
+    a = (od.od_q4_logits(ctx, x, codes, scales).double() * dy.double()).sum()
+    b = (od.od_q4_logits_grad(ctx, dy, codes, scales).double() * x.double()).sum()
+    w = weights(codes, scales)
+    size = float((x.double().abs() @ w.abs().T * dy.double().abs()).sum())
+    assert abs(float(a - b)) <= size * (2.0 ** -17 + math.ceil(V / 16) * 3 * 2.0 ** -22)
+
+
+def test_codes_past_32_bits(ctx):
+    """More than 2^32 weights, a token's worth of them checked."""
+    V, H, G = 70000, 65536, 128
+    codes = torch.randint(0, 256, (V, H // 2), device="cuda", dtype=torch.uint8)
+    scales = torch.ones(V, H // G, dtype=BF16, device="cuda") / 16
+    x = torch.randn(1, H, device="cuda").to(BF16)
+    y = od.od_q4_logits(ctx, x, codes, scales)
+    rows = torch.tensor([0, 1, 32767, 32768, 65535, 65536, 69998, V - 1], device="cuda")
+    check_logits(y[:, rows], x, weights(codes[rows], scales[rows]), G)
+    dy = padded(torch.zeros(1, V, device="cuda"))
+    dy[0, rows] = torch.randn(len(rows), device="cuda")
+    check_grad(od.od_q4_logits_grad(ctx, dy, codes, scales), dy[:, rows], weights(codes[rows], scales[rows]))
+
+
+def test_batches_of_rows_captured_and_replayed_on_another_stream(ctx):
+    B, K, V, H, G = 3, 4, 1500, 512, 128
+    codes, scales = layer(V, H, G, 7)
+    w = weights(codes, scales)
+    x = torch.randn(B, K, H, device="cuda").to(BF16)
+    logits = padded(torch.zeros(B, K, V, device="cuda"))
+    back = torch.empty(B, K, H, device="cuda")
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        od.od_q4_logits(ctx, x, codes, scales, out=logits)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            od.od_q4_logits(ctx, x, codes, scales, out=logits)
+            od.od_q4_logits_grad(ctx, logits, codes, scales, out=back)
+        x.copy_(torch.randn(B, K, H, device="cuda"))
+        graph.replay()
+    torch.cuda.synchronize()
+    check_logits(logits.reshape(-1, V), x.view(-1, H), w, G)
+    check_grad(back.view(-1, H), logits.reshape(-1, V), w)
+
+
+def test_a_training_step_of_the_drafter(ctx):
+    """Hidden states -> logits -> scores -> the gradient of a loss on them -> the hidden states' gradient, against autograd in 64 bits."""
+    B, K, V, H, G, n = 3, 5, 3001, 256, 64, 4
+    codes, scales = layer(V, H, G, 8)
+    scales = (scales.float() / 64).to(BF16)
+    w = weights(codes, scales)
+    hidden = torch.randn(B, K, H, device="cuda").to(BF16)
+    T = torch.tensor([1.0, 0.7, 0.5], device="cuda")
+    ids = torch.randint(0, V, (B, K), device="cuda", dtype=torch.int32)
+    n_rows = torch.tensor([5, 3, 4], dtype=torch.int32, device="cuda")
+    live = torch.arange(K, device="cuda")[None] < n_rows[:, None]
+    logits = od.od_q4_logits(ctx, hidden, codes, scales)
+    lp = od.od_token_logprobs(ctx, logits, ids, T, n_rows, n)
+    a, b = torch.randn(B, K, device="cuda"), torch.randn(B, K, device="cuda")
+    c = torch.randn(B, K, n, device="cuda")
+    g_logits = od.od_token_logprobs_grad(ctx, logits, ids, lp, a, b, c, T, n_rows)
+    got = od.od_q4_logits_grad(ctx, g_logits, codes, scales)
+    h = hidden.double().requires_grad_()
+    ref = torch.log_softmax(h @ w.T / T.double()[:, None, None], 2)
+    top = torch.gather(ref, 2, torch.where(live[:, :, None], lp.top_ids, 0).long())
+    assert torch.equal(lp.top_ids[live].long(), torch.topk(ref, n, dim=2).indices[live])
+    loss = (a * torch.gather(ref, 2, ids.long()[:, :, None]).squeeze(2) - b * (ref.exp() * ref).sum(2) + (c * top).sum(2))[live].sum()
+    loss.backward()
+    # the logits' errors (group sums of |x w|) through a softmax, then the tolerances of the two gradients
+    size = float((hidden.double().abs() @ w.abs().T).max())
+    spread = (a.abs() + 16 * b.abs() + c.abs().sum(2)).double()[:, :, None] * w.abs().max() * 2 / T.double()[:, None, None]
+    tol = spread * (size * 2.0 ** -18 * 4 + 2.0 ** -14)
+    assert ((got.double() - h.grad).abs() <= tol)[live].all()
+    assert not got[~live].any()
+
+
+def test_refusals(ctx):
+    codes, scales = layer(100, 128, 32, 9)
+    x = torch.randn(2, 128, device="cuda")
+    od.od_q4_logits(ctx, x, codes, scales)
+    with pytest.raises(TypeError):
+        od.od_q4_logits(ctx, x.half(), codes, scales)
+    with pytest.raises(TypeError):
+        od.od_q4_logits(ctx, x, codes.int(), scales)
+    with pytest.raises(TypeError):
+        od.od_q4_logits(ctx, x, codes, scales.float())
+    with pytest.raises(ValueError):
+        od.od_q4_logits(ctx, x[:, :64], codes, scales)
+    with pytest.raises(ValueError):
+        od.od_q4_logits(ctx, x, codes, scales[:50])
+    with pytest.raises(ValueError):
+        od.od_q4_logits(ctx, x, codes[:, ::2], scales)
+    with pytest.raises(ValueError):
+        od.od_q4_logits(ctx, x, codes, scales, out=torch.empty(3, 100, device="cuda"))
+    with pytest.raises(ValueError):
+        od.od_q4_logits(ctx, x.cpu(), codes, scales)
+    with pytest.raises(ValueError):                         # rows that are not equally far apart
+        od.od_q4_logits(ctx, torch.zeros(2, 3, 128, device="cuda")[:, :2], codes, scales)
+    with pytest.raises(od.OdError) as e:
+        od.od_q4_logits(ctx, x, codes, torch.zeros(100, 128 // 16, dtype=BF16, device="cuda"))
+    assert e.value.status == od.OD_ERR_UNSUPPORTED
+    with pytest.raises(od.OdError) as e:
+        od.od_q4_logits(ctx, x, torch.zeros(100 * 64 + 1, dtype=torch.uint8, device="cuda")[1:].view(100, 64), scales)
+    assert e.value.status == od.OD_ERR_ALIGNMENT
+    with pytest.raises(od.OdError) as e:
+        od.od_q4_logits(ctx, x, codes, scales, out=torch.empty(2, 101, device="cuda")[:, :100])
+    assert e.value.status == od.OD_ERR_ALIGNMENT
+    assert od.od_q4_logits(ctx, x[:0], codes, scales).shape == (0, 100)
+    assert od.od_q4_logits_grad(ctx, torch.zeros(0, 100, device="cuda"), codes, scales).shape == (0, 128)
