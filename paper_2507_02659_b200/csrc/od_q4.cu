@@ -1,105 +1,529 @@
 // An output layer with 4-bit weights, for a few tokens, and the way of a gradient back through it:
 //   w[v,h] = s[v, h / G] (u[v,h] - 8),   y[n,v] = sum_h x[n,h] w[v,h],   dx[n,h] = sum_v dy[n,v] w[v,h].
-// Codes u are 4 bits (column 2i in the low half of byte i of a row), scales s are bf16. Products and sums are fp32.
+// Codes u are 4 bits (column 2i in the low half of byte i of a row), scales s are bf16.
+//
+// Both products run on the tensor pipe as mma.m16n8k16 with the codes as the first operand and eight tokens as the
+// second. u - 8 is exact in bf16, and so is an input: a bf16 one as it is, an fp32 one as the sum of three bf16 pieces
+// (24 bits = 8 + 8 + 8), the product of a bf16 gradient and a bf16 scale as that of two. So the only roundings are those
+// of fp32 sums (and of an fp32 gradient times its scale). The scale of a group belongs to a row of the weights: forward
+// it multiplies the group's sum, backward, where rows are summed over, the gradient.
+//
+// For a few tokens the codes are all there is to move; what competes with them is unpacking: 11 instructions for eight
+// codes (three shifts, four masks that put a code into the low mantissa bits of bf16 128, four subtractions of 136).
+// That is why the operands go from registers straight into mma.sync and not through shared memory to tcgen05, whose
+// operands would be written and read there once more at two bytes a weight.
+//
+// A warp streams its own codes through a ring of 1 KB stages in shared memory (16 rows x 128 columns, cp.async), so that
+// no block barrier holds it up; sixteen-byte pieces are placed so that the words of a fragment lie in different banks.
+#include <float.h>
+
 #include "od_common.cuh"
 
 namespace {
 
-constexpr int TOKENS = 8;                                  // of a block
+constexpr int WARPS = 16, THREADS = 32 * WARPS;
+constexpr int ROWS = 16;                                   // of a stage, and of a matrix instruction
+constexpr int COLS = 128;                                  // of a stage: four blocks of 32
+constexpr int STAGE = ROWS * COLS / 2;                     // bytes
+constexpr int RING = 6;                                    // stages of a warp
+constexpr int MAX_SPLIT = OD_Q4_MAX_SPLIT;                 // blocks that share the rows of a gradient (a cluster)
 
-template <typename T> __device__ __forceinline__ float to_float(T v);
-template <> __device__ __forceinline__ float to_float<float>(float v) { return v; }
-template <> __device__ __forceinline__ float to_float<unsigned short>(unsigned short v) { return __uint_as_float((uint32_t)v << 16); }
-template <typename T> __device__ __forceinline__ T from_float(float v);
-template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
-template <> __device__ __forceinline__ unsigned short from_float<unsigned short>(float v)
+struct Q4Args {
+    const void *in;                                        // x or dy
+    int64_t in_stride;
+    const uint8_t *codes;
+    const unsigned short *scales;
+    void *out;
+    int64_t out_stride;
+    int32_t N, V, H, in_f32, out_f32;
+    int32_t wide_scales;                                   // the scales of a stage's row are one aligned word
+    int32_t split, col_warps;                              // backward: blocks of a cluster, warps side by side
+};
+
+__device__ __forceinline__ void cp16(uint32_t to, const void *from)
 {
-    uint32_t d;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(0.f), "f"(v));
-    return (unsigned short)d;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ uint32_t lds32(uint32_t at)
+{
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ float lds_cluster(uint32_t at)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// codes i and i + 4 of a word, less 8, as a pair of bf16: 128 + u has u in its last bits
+template <int I>
+__device__ __forceinline__ uint32_t unpack(uint32_t w)
+{
+    uint32_t m = ((w >> 4 * I) & 0x000F000Fu) | 0x43004300u, d;
+    asm("sub.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(m), "r"(0x43084308u));
+    return d;
+}
+__device__ __forceinline__ uint32_t halves(uint32_t a, uint32_t b, uint32_t pick)
+{
+    return __byte_perm(a, b, pick);
+}
+constexpr uint32_t LOW = 0x5410, HIGH = 0x7632;            // both low halves, both high halves
+
+// x = hi + mid + lo by cutting its bits; of an infinity everything is in hi
+__device__ __forceinline__ void cut(float x, bool guard, float &rest)
+{
+    rest = x - __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
+    if (guard && fabsf(x) == INFINITY) rest = 0.f;
+}
+// P pieces of a pair as bf16 pairs
+template <int P>
+__device__ __forceinline__ void pieces(float a, float b, bool guard, uint32_t (&out)[P])
+{
+    out[0] = halves(__float_as_uint(a), __float_as_uint(b), HIGH);
+#pragma unroll
+    for (int p = 1; p < P; ++p) {
+        cut(a, guard, a);
+        cut(b, guard, b);
+        out[p] = halves(__float_as_uint(a), __float_as_uint(b), HIGH);
+    }
 }
 
-// a warp to a row of the weights
-template <typename X, typename Y>
-__global__ void od_q4_kernel(int N, int V, int H, int log_g, const X *x, int64_t xs, const uint8_t *codes, const unsigned short *scales,
-                             Y *y, int64_t ys)
+__device__ __forceinline__ void store(const Q4Args &A, int n, int i, float v)
 {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int lane = threadIdx.x & 31, v = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5), n0 = blockIdx.y * TOKENS;
-    if (v >= V) return;
-    float acc[TOKENS] = {};
-    for (int i = lane; i < H / 2; i += 32) {
-        const uint8_t q = codes[(size_t)v * (H / 2) + i];
-        const float s = to_float(scales[(size_t)v * (H >> log_g) + (2 * i >> log_g)]);
-        const float lo = s * (float)((q & 15) - 8), hi = s * (float)((q >> 4) - 8);
-#pragma unroll
-        for (int t = 0; t < TOKENS; ++t)
-            if (n0 + t < N) acc[t] += lo * to_float(x[(n0 + t) * xs + 2 * i]) + hi * to_float(x[(n0 + t) * xs + 2 * i + 1]);
-    }
-#pragma unroll
-    for (int t = 0; t < TOKENS; ++t) {
-#pragma unroll
-        for (int o = 16; o; o >>= 1) acc[t] += __shfl_xor_sync(0xFFFFFFFFu, acc[t], o);
-        if (lane == 0 && n0 + t < N) y[(n0 + t) * ys + v] = from_float<Y>(acc[t]);
+    if (A.out_f32) {
+        ((float *)A.out)[(size_t)n * A.out_stride + i] = v;
+    } else {
+        uint32_t d;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(0.f), "f"(v));
+        ((unsigned short *)A.out)[(size_t)n * A.out_stride + i] = (unsigned short)d;
     }
 }
 
-// a thread to two columns of the weights
-template <typename X, typename Y>
-__global__ void od_q4_grad_kernel(int N, int V, int H, int log_g, const X *dy, int64_t ds, const uint8_t *codes,
-                                  const unsigned short *scales, Y *dx, int64_t xs)
-{
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int i = blockIdx.x * blockDim.x + threadIdx.x, n0 = blockIdx.y * TOKENS;
-    if (i >= H / 2) return;
-    float lo[TOKENS] = {}, hi[TOKENS] = {};
-    for (int v = 0; v < V; ++v) {
-        const uint8_t q = codes[(size_t)v * (H / 2) + i];
-        const float s = to_float(scales[(size_t)v * (H >> log_g) + (2 * i >> log_g)]);
+// The scales of a stage's columns in one row of the weights, raw: 4 / GB of them in the first halves of two words.
+template <int GB>
+struct Scales {
+    uint32_t w[GB == 1 ? 2 : 1];
+    // at: the row's first scale of the stage; n: how many of them there are
+    __device__ __forceinline__ void load(const unsigned short *at, int n, bool wide)
+    {
+        if (GB == 4) {
+            w[0] = __ldg(at);
+        } else if (wide) {
+            if constexpr (GB == 1) {
+                const uint2 v = __ldg((const uint2 *)at);
+                w[0] = v.x; w[1] = v.y;
+            } else {
+                w[0] = __ldg((const uint32_t *)at);
+            }
+        } else {
 #pragma unroll
-        for (int t = 0; t < TOKENS; ++t) {
-            if (n0 + t >= N) continue;
-            const float g = s * to_float(dy[(n0 + t) * ds + v]);
-            lo[t] += g * (float)((q & 15) - 8);
-            hi[t] += g * (float)((q >> 4) - 8);
+            for (int i = 0; i < 4 / GB; i += 2) {
+                const uint32_t lo = i < n ? __ldg(at + i) : 0u, hi = i + 1 < n ? __ldg(at + i + 1) : 0u;
+                w[i / 2] = lo | hi << 16;
+            }
         }
     }
+    __device__ __forceinline__ float get(int i) const { return i & 1 ? od_bf16_hi(w[i >> 1]) : od_bf16_lo(w[i >> 1]); }
+    __device__ __forceinline__ void clear()
+    {
 #pragma unroll
-    for (int t = 0; t < TOKENS; ++t) {
-        if (n0 + t >= N) break;
-        dx[(n0 + t) * xs + 2 * i] = from_float<Y>(lo[t]);
-        dx[(n0 + t) * xs + 2 * i + 1] = from_float<Y>(hi[t]);
+        for (auto &x : w) x = 0;
     }
+};
+
+// ---- forward: 16 rows of the weights to a warp, all columns -------------------------------------
+//
+// A word of a row is eight columns: a stage's block of 32 columns is four words, one to each of the four lanes that share
+// a row of the fragment, and codes i and i + 4 of the word are its pairs. The lanes' inputs are the same eight columns:
+// sixteen (bf16) or thirty-two (fp32) bytes, read through L1 where the block's warps share them.
+template <int P, int NT, int GB>
+__global__ void __launch_bounds__(THREADS, 1) od_q4_kernel(const Q4Args A)
+{
+    extern __shared__ __align__(128) unsigned char smem[];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const int H = A.H, V = A.V, blocks = H / 32, stages = (blocks + 3) / 4, n_groups = blocks / GB;
+    const int n0 = blockIdx.y * (8 * NT);
+    const int units = (V + ROWS - 1) / ROWS, step = gridDim.x * WARPS;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (RING * STAGE);
+    const size_t row_bytes = (size_t)H / 2;
+
+    // fetching: this lane copies piece lane % 4 of rows lane / 4 and 8 + lane / 4
+    int fu = blockIdx.x + warp * gridDim.x, fs = 0, slot_f = 0;
+    const uint32_t put = ring + (lane >> 2) * 64 + ((t ^ ((lane >> 3) & 3)) << 4);
+    const uint8_t *f0 = nullptr, *f1 = nullptr;
+    auto aim = [&]() {
+        const int r = fu * ROWS + (lane >> 2);
+        f0 = A.codes + min(r, V - 1) * row_bytes + t * 16;
+        f1 = A.codes + min(r + 8, V - 1) * row_bytes + t * 16;
+    };
+    auto fetch = [&]() {
+        if (fu < units) {
+            if (fs == 0) aim();
+            if (fs * 4 + t < blocks) {
+                cp16(put + slot_f * STAGE, f0 + (size_t)fs * 64);
+                cp16(put + slot_f * STAGE + 8 * 64, f1 + (size_t)fs * 64);
+            }
+            if (++fs == stages) { fs = 0; fu += step; }
+        }
+        cp_commit();
+        slot_f = slot_f + 1 == RING ? 0 : slot_f + 1;
+    };
+#pragma unroll
+    for (int i = 0; i < RING - 1; ++i) fetch();
+
+    const uint32_t get = ring + g * 64 + t * 4;
+    const int swz = (g >> 1) & 3;
+    const char *x[NT];
+    bool has[NT];
+#pragma unroll
+    for (int q = 0; q < NT; ++q) {
+        has[q] = n0 + q * 8 + g < A.N;
+        x[q] = (const char *)A.in + ((int64_t)(has[q] ? n0 + q * 8 + g : 0) * A.in_stride + t * 8) * (P == 1 ? 2 : 4);
+    }
+    int slot = 0;
+    Scales<GB> s0, s1, next0, next1;
+    auto load_scales = [&](int u, int s) {
+        const int r = u * ROWS + g, i = s * (4 / GB);
+        next0.load(A.scales + (size_t)min(r, V - 1) * n_groups + i, n_groups - i, A.wide_scales);
+        next1.load(A.scales + (size_t)min(r + 8, V - 1) * n_groups + i, n_groups - i, A.wide_scales);
+    };
+    int u = blockIdx.x + warp * gridDim.x;
+    if (u < units) load_scales(u, 0);
+    for (; u < units; u += step) {
+        float total[NT][4] = {}, sum[NT][4];
+        for (int s = 0; s < stages; ++s) {
+            s0 = next0; s1 = next1;
+            if (s + 1 < stages) load_scales(u, s + 1);
+            else if (u + step < units) load_scales(u + step, 0);
+            cp_wait<RING - 2>();
+            __syncwarp();
+            fetch();
+            const int here = min(4, blocks - s * 4);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (j >= here) break;
+                uint32_t b[NT][4][P];
+#pragma unroll
+                for (int q = 0; q < NT; ++q) {
+                    const char *at = x[q] + (size_t)(s * 4 + j) * 32 * (P == 1 ? 2 : 4);
+                    if constexpr (P == 1) {
+                        uint4 v = make_uint4(0, 0, 0, 0);
+                        if (has[q]) v = __ldg((const uint4 *)at);
+                        b[q][0][0] = halves(v.x, v.z, LOW); b[q][1][0] = halves(v.x, v.z, HIGH);
+                        b[q][2][0] = halves(v.y, v.w, LOW); b[q][3][0] = halves(v.y, v.w, HIGH);
+                    } else {
+                        float4 v = make_float4(0.f, 0.f, 0.f, 0.f), w = v;
+                        if (has[q]) { v = __ldg((const float4 *)at); w = __ldg((const float4 *)at + 1); }
+                        const float m = fmaxf(fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w))),
+                                              fmaxf(fmaxf(fabsf(w.x), fabsf(w.y)), fmaxf(fabsf(w.z), fabsf(w.w))));
+                        const bool guard = __any_sync(0xFFFFFFFFu, m == INFINITY);
+                        pieces<P>(v.x, w.x, guard, b[q][0]); pieces<P>(v.y, w.y, guard, b[q][1]);
+                        pieces<P>(v.z, w.z, guard, b[q][2]); pieces<P>(v.w, w.w, guard, b[q][3]);
+                    }
+                }
+                const uint32_t at = get + slot * STAGE + ((j ^ swz) << 4);
+                const uint32_t w0 = lds32(at), w1 = lds32(at + 8 * 64);
+                const uint32_t a0[4] = {unpack<0>(w0), unpack<0>(w1), unpack<1>(w0), unpack<1>(w1)};
+                const uint32_t a1[4] = {unpack<2>(w0), unpack<2>(w1), unpack<3>(w0), unpack<3>(w1)};
+#pragma unroll
+                for (int q = 0; q < NT; ++q) {
+                    if (j % GB == 0) sum[q][0] = sum[q][1] = sum[q][2] = sum[q][3] = 0.f;
+#pragma unroll
+                    for (int p = 0; p < P; ++p) {
+                        mma(sum[q], a0, b[q][0][p], b[q][1][p]);
+                        mma(sum[q], a1, b[q][2][p], b[q][3][p]);
+                    }
+                    if (j % GB == GB - 1) {
+                        const float e0 = s0.get(j / GB), e1 = s1.get(j / GB);
+                        total[q][0] = fmaf(e0, sum[q][0], total[q][0]); total[q][1] = fmaf(e0, sum[q][1], total[q][1]);
+                        total[q][2] = fmaf(e1, sum[q][2], total[q][2]); total[q][3] = fmaf(e1, sum[q][3], total[q][3]);
+                    }
+                }
+            }
+            slot = slot + 1 == RING ? 0 : slot + 1;
+        }
+#pragma unroll
+        for (int q = 0; q < NT; ++q)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int n = n0 + q * 8 + 2 * t + (k & 1), v = u * ROWS + g + (k >> 1) * 8;
+                if (n < A.N && v < V) store(A, n, v, total[q][k]);
+            }
+    }
+    cp_wait<0>();
 }
 
-template <typename X, typename Y>
-cudaError_t launch(bool backward, int32_t N, int32_t V, int32_t H, int log_g, const void *a, int64_t as, const void *codes,
-                   const void *scales, void *b, int64_t bs, bool pdl, cudaStream_t s)
+// ---- backward: 128 columns to a warp, every so many-th 16 rows ----------------------------------
+//
+// Rows are summed over: two of them are the pair of an operand, four columns in a row are a half word, so a block of 32
+// columns is the sixteen rows of two fragments. A lane reads the word that its half is in of four rows. The tokens' side is
+// made anew for each group: gradient times scale, in pieces. Warps side by side share rows (a block reads up to 256
+// bytes in a row); those on the same columns, and the blocks of a cluster, are summed at the end in a fixed order.
+template <int P, int NT, int GB>
+__global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
 {
-    cudaLaunchConfig_t cfg = {};
-    const unsigned tiles = (unsigned)((N + TOKENS - 1) / TOKENS);
-    cfg.blockDim = dim3(128);
-    cfg.gridDim = backward ? dim3((unsigned)((H / 2 + 127) / 128), tiles) : dim3((unsigned)((V + 3) / 4), tiles);
-    cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr; cfg.numAttrs = pdl ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, backward ? od_q4_grad_kernel<X, Y> : od_q4_kernel<X, Y>, (int)N, (int)V, (int)H, log_g, (const X *)a, as,
-                              (const uint8_t *)codes, (const unsigned short *)scales, (Y *)b, bs);
+    extern __shared__ __align__(128) unsigned char smem[];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const int H = A.H, V = A.V, cw = A.col_warps, split = A.split;
+    const int rank = blockIdx.x % split, tile = blockIdx.x / split;
+    const int col = (tile * cw + warp % cw) * COLS, here = max(0, min(4, (H - col) / 32)), n_groups = H / (32 * GB);
+    const int slabs = split * (WARPS / cw), slab = rank * (WARPS / cw) + warp / cw;
+    const int steps = here > 0 ? (V + ROWS - 1) / ROWS : 0, n0 = blockIdx.y * (8 * NT);
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (RING * STAGE);
+    const size_t row_bytes = (size_t)H / 2;
+
+    int fs = slab, slot_f = 0;
+    const uint32_t put = ring + (lane >> 2) * 64 + ((t ^ (lane >> 4)) << 4), put8 = ring + (8 + (lane >> 2)) * 64 + ((t ^ (2 + (lane >> 4))) << 4);
+    const uint8_t *from = A.codes + (size_t)col / 2 + t * 16;
+    auto fetch = [&]() {
+        if (fs < steps) {
+            const int r = fs * ROWS + (lane >> 2);
+            if (t < here) {
+                cp16(put + slot_f * STAGE, from + min(r, V - 1) * row_bytes);
+                cp16(put8 + slot_f * STAGE, from + min(r + 8, V - 1) * row_bytes);
+            }
+            fs += slabs;
+        }
+        cp_commit();
+        slot_f = slot_f + 1 == RING ? 0 : slot_f + 1;
+    };
+#pragma unroll
+    for (int i = 0; i < RING - 1; ++i) fetch();
+
+    // a lane's words: rows 4t .. 4t + 3, word g / 2 of a block's piece (pieces of these rows are placed by t)
+    const uint32_t get = ring + 4 * t * 64 + (g >> 1) * 4, pick = g & 1 ? HIGH : LOW;
+    const char *dy[NT];
+    bool has[NT];
+#pragma unroll
+    for (int q = 0; q < NT; ++q) {
+        has[q] = n0 + q * 8 + g < A.N;
+        dy[q] = (const char *)A.in + ((int64_t)(has[q] ? n0 + q * 8 + g : 0) * A.in_stride + 4 * t) * (P == 2 ? 2 : 4);
+    }
+    Scales<GB> sc[4], next_sc[4];
+    float d[NT][4], next_d[NT][4];
+    auto load = [&](int s) {
+        const int r = s * ROWS + 4 * t, i = col / (32 * GB);
+        const unsigned short *at = A.scales + (size_t)r * n_groups + i;
+        const bool whole = s * ROWS + ROWS <= V;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (whole || r + k < V) next_sc[k].load(at + (size_t)k * n_groups, n_groups - i, A.wide_scales);
+            else next_sc[k].clear();                       // (zero times a gradient of zero)
+        }
+#pragma unroll
+        for (int q = 0; q < NT; ++q) {
+            const char *p = dy[q] + (size_t)s * ROWS * (P == 2 ? 2 : 4);
+            if (!has[q]) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) next_d[q][k] = 0.f;
+            } else if (whole) {
+                if constexpr (P == 2) {
+                    const uint2 v = __ldg((const uint2 *)p);
+                    next_d[q][0] = od_bf16_lo(v.x); next_d[q][1] = od_bf16_hi(v.x);
+                    next_d[q][2] = od_bf16_lo(v.y); next_d[q][3] = od_bf16_hi(v.y);
+                } else {
+                    const float4 v = __ldg((const float4 *)p);
+                    next_d[q][0] = v.x; next_d[q][1] = v.y; next_d[q][2] = v.z; next_d[q][3] = v.w;
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    next_d[q][k] = 0.f;
+                    if (r + k < V) next_d[q][k] = P == 2 ? __uint_as_float((uint32_t)__ldg((const unsigned short *)p + k) << 16) : __ldg((const float *)p + k);
+                }
+            }
+        }
+    };
+    float acc[8][NT][4] = {};
+    int slot = 0;
+    if (slab < steps) load(slab);
+    for (int s = slab; s < steps; s += slabs) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sc[k] = next_sc[k];
+#pragma unroll
+        for (int q = 0; q < NT; ++q)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) d[q][k] = next_d[q][k];
+        if (s + slabs < steps) load(s + slabs);
+        cp_wait<RING - 2>();
+        __syncwarp();
+        fetch();
+        uint32_t b[NT][2][P];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (j >= here) break;
+            if (j % GB == 0) {
+#pragma unroll
+                for (int q = 0; q < NT; ++q) {
+                    float z[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) z[k] = d[q][k] * sc[k].get(j / GB);
+                    const float m = fmaxf(fmaxf(fabsf(z[0]), fabsf(z[1])), fmaxf(fabsf(z[2]), fabsf(z[3])));
+                    const bool guard = __any_sync(0xFFFFFFFFu, m == INFINITY);
+                    pieces<P>(z[0], z[1], guard, b[q][0]);
+                    pieces<P>(z[2], z[3], guard, b[q][1]);
+                }
+            }
+            const uint32_t at = get + slot * STAGE + ((j ^ t) << 4);
+            const uint32_t w01 = halves(lds32(at), lds32(at + 64), pick), w23 = halves(lds32(at + 128), lds32(at + 192), pick);
+            const uint32_t a0[4] = {unpack<0>(w01), unpack<1>(w01), unpack<0>(w23), unpack<1>(w23)};
+            const uint32_t a1[4] = {unpack<2>(w01), unpack<3>(w01), unpack<2>(w23), unpack<3>(w23)};
+#pragma unroll
+            for (int q = 0; q < NT; ++q)
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    mma(acc[2 * j][q], a0, b[q][0][p], b[q][1][p]);
+                    mma(acc[2 * j + 1][q], a1, b[q][0][p], b[q][1][p]);
+                }
+        }
+        slot = slot + 1 == RING ? 0 : slot + 1;
+    }
+    cp_wait<0>();
+    __syncthreads();                                       // the rings are free
+
+    // [warp][token][column]; the warps on the same columns are summed into the first of them
+    constexpr int PART = 8 * NT * COLS;                    // numbers of a warp
+    float *part = (float *)smem;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+            for (int q = 0; q < NT; ++q)
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    *(float2 *)(part + warp * PART + (q * 8 + 2 * t + k) * COLS + 32 * j + 4 * g + 2 * a) =
+                        make_float2(acc[2 * j + a][q][k], acc[2 * j + a][q][k + 2]);
+    __syncthreads();
+    const int n_sums = cw * PART;
+    for (int i = threadIdx.x; i < n_sums; i += THREADS) {
+        float v = part[i];
+        for (int w = cw; w < WARPS; w += cw) v += part[w * PART + i];
+        part[i] = v;
+    }
+    __syncthreads();
+    if (split > 1) { od_cluster_arrive(); od_cluster_wait(); }
+    // and the blocks of the cluster, each a share of the columns
+    for (int i = (int)((int64_t)n_sums * rank / split) + threadIdx.x; i < (int)((int64_t)n_sums * (rank + 1) / split); i += THREADS) {
+        const int n = n0 + i % PART / COLS, h = (tile * cw + i / PART) * COLS + i % COLS;
+        float v = 0.f;
+        for (int r = 0; r < split; ++r) v += split > 1 ? lds_cluster(od_cluster_address(part + i, r)) : part[i];
+        if (n < A.N && h < H) store(A, n, h, v);
+    }
+    if (split > 1) { od_cluster_arrive(); od_cluster_wait(); }
+}
+
+constexpr int ring_bytes = WARPS * RING * STAGE;
+template <int NT> constexpr int grad_bytes = WARPS * 8 * NT * COLS * 4 > ring_bytes ? WARPS * 8 * NT * COLS * 4 : ring_bytes;
+
+typedef void (*Kernel)(Q4Args);
+struct Variant { Kernel kernel; int smem, tokens; };
+
+// by log2(group / 32); forward: tokens of a block by 8, 16, 32 (fp32 inputs: 8), backward: by 8, 16
+template <int GB>
+Variant forward_of(bool f32, int N)
+{
+    if (f32) return {od_q4_kernel<3, 1, GB>, ring_bytes, 8};
+    if (N <= 8) return {od_q4_kernel<1, 1, GB>, ring_bytes, 8};
+    return N <= 16 ? Variant{od_q4_kernel<1, 2, GB>, ring_bytes, 16} : Variant{od_q4_kernel<1, 4, GB>, ring_bytes, 32};
+}
+template <int GB>
+Variant backward_of(bool f32, int N)
+{
+    if (f32) return N <= 8 ? Variant{od_q4_grad_kernel<3, 1, GB>, grad_bytes<1>, 8} : Variant{od_q4_grad_kernel<3, 2, GB>, grad_bytes<2>, 16};
+    return N <= 8 ? Variant{od_q4_grad_kernel<2, 1, GB>, grad_bytes<1>, 8} : Variant{od_q4_grad_kernel<2, 2, GB>, grad_bytes<2>, 16};
+}
+Variant variant(bool backward, int32_t G, bool f32, int N)
+{
+    if (backward) return G == 32 ? backward_of<1>(f32, N) : G == 64 ? backward_of<2>(f32, N) : backward_of<4>(f32, N);
+    return G == 32 ? forward_of<1>(f32, N) : G == 64 ? forward_of<2>(f32, N) : forward_of<4>(f32, N);
+}
+
+void configure(cudaLaunchConfig_t &cfg, cudaLaunchAttribute (&attr)[2], const Variant &v, unsigned blocks, unsigned tiles, unsigned cluster)
+{
+    cfg = {};
+    cfg.gridDim = dim3(blocks, tiles); cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = v.smem;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
 }
 
 }  // namespace
 
+// the kernels' limits; clusters[0 / 1][n]: clusters of n blocks that are resident at a time, up to 8 / more tokens
+cudaError_t od_q4_prepare_device(int32_t (*clusters)[OD_Q4_MAX_SPLIT + 1])
+{
+    for (int backward = 0; backward < 2; ++backward)
+        for (int32_t G = 32; G <= 128; G *= 2)
+            for (int f32 = 0; f32 < 2; ++f32)
+                for (int N = 8; N <= 32; N *= 2) {
+                    const Variant v = variant(backward, G, f32, N);
+                    cudaError_t e = cudaFuncSetAttribute((const void *)v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, v.smem);
+                    if (e == cudaSuccess && backward) e = cudaFuncSetAttribute((const void *)v.kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+                    if (e != cudaSuccess) return e;
+                }
+    for (int wide = 0; wide < 2; ++wide)
+        for (int n = 1; n <= MAX_SPLIT; ++n) {
+            cudaLaunchConfig_t cfg;
+            cudaLaunchAttribute attr[2];
+            const Variant v = variant(true, 32, true, wide ? 16 : 8);
+            configure(cfg, attr, v, (unsigned)n, 1, (unsigned)n);
+            int here = 0;
+            if (cudaOccupancyMaxActiveClusters(&here, (const void *)v.kernel, &cfg) != cudaSuccess) {
+                cudaGetLastError();
+                here = 0;
+            }
+            clusters[wide][n] = here;
+        }
+    return cudaSuccess;
+}
+
 cudaError_t od_launch_q4(const od_ctx *c, bool backward, int32_t N, int32_t V, int32_t H, int32_t G, const void *a, int32_t a_dtype,
                          int64_t as, const void *codes, const void *scales, void *b, int32_t b_dtype, int64_t bs, cudaStream_t s)
 {
-    const int log_g = G == 32 ? 5 : G == 64 ? 6 : 7;
-    const bool pdl = c->opt_pdl != 0;
-    typedef unsigned short bf16;
-    if (a_dtype == OD_BF16)
-        return b_dtype == OD_BF16 ? launch<bf16, bf16>(backward, N, V, H, log_g, a, as, codes, scales, b, bs, pdl, s)
-                                  : launch<bf16, float>(backward, N, V, H, log_g, a, as, codes, scales, b, bs, pdl, s);
-    return b_dtype == OD_BF16 ? launch<float, bf16>(backward, N, V, H, log_g, a, as, codes, scales, b, bs, pdl, s)
-                              : launch<float, float>(backward, N, V, H, log_g, a, as, codes, scales, b, bs, pdl, s);
+    const Variant v = variant(backward, G, a_dtype == OD_F32, N);
+    Q4Args args = {a, as, (const uint8_t *)codes, (const unsigned short *)scales, b, bs, N, V, H, a_dtype == OD_F32, b_dtype == OD_F32,
+                   H % COLS == 0 && ((uintptr_t)scales & 7u) == 0, 1, 1};
+    unsigned blocks;
+    if (!backward) {
+        const int64_t units = ((int64_t)V + ROWS - 1) / ROWS;
+        blocks = (unsigned)(units < c->sm_count ? units : c->sm_count);
+    } else {
+        // How many warps side by side (4, 2, 1) and blocks to a cluster (any number that the device holds): the fewest
+        // rounds of clusters times rows of a warp; of equal ones the widest rows.
+        const int32_t *resident = c->q4_clusters[v.tokens > 8];
+        int64_t best = INT64_MAX;
+        int32_t tiles_of = 1;
+        for (int32_t cw = 4; cw >= 1; cw /= 2)
+            for (int32_t n = 1; n <= MAX_SPLIT; ++n) {
+                if (resident[n] < 1) continue;
+                const int32_t tiles = (H + cw * COLS - 1) / (cw * COLS);
+                const int64_t rounds = (tiles + resident[n] - 1) / resident[n];
+                const int64_t cost = rounds * ((V + ROWS - 1) / ROWS + n * (WARPS / cw) - 1) / (n * (WARPS / cw));
+                if (cost < best) { best = cost; args.col_warps = cw; args.split = n; tiles_of = tiles; }
+            }
+        blocks = (unsigned)(tiles_of * args.split);
+    }
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[2];
+    configure(cfg, attr, v, blocks, (unsigned)((N + v.tokens - 1) / v.tokens), (unsigned)args.split);
+    cfg.stream = s;
+    cfg.numAttrs = c->opt_pdl ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, v.kernel, args);
 }
