@@ -143,97 +143,140 @@ struct Scales {
 // ---- forward: 16 rows of the weights to a warp, all columns -------------------------------------
 //
 // A word of a row is eight columns: a stage's block of 32 columns is four words, one to each of the four lanes that share
-// a row of the fragment, and codes i and i + 4 of the word are its pairs. The lanes' inputs are the same eight columns:
-// sixteen (bf16) or thirty-two (fp32) bytes, read through L1 where the block's warps share them.
-template <int P, int NT, int GB>
+// a row of the fragment, and codes i and i + 4 of the word are its pairs. The lanes' inputs are the same eight columns of
+// a token. XS: a block of threads keeps its tokens' inputs in shared memory as the words of the fragments, 16 bytes to a
+// lane; where they do not fit, they are read and cut again for every 16 rows.
+
+// the words of a lane's fragments for eight columns of a token
+template <int P>
+__device__ __forceinline__ void load_inputs(const char *at, bool has, uint32_t (&b)[P][4])
+{
+    if constexpr (P == 1) {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (has) v = __ldg((const uint4 *)at);
+        b[0][0] = halves(v.x, v.z, LOW); b[0][1] = halves(v.x, v.z, HIGH);
+        b[0][2] = halves(v.y, v.w, LOW); b[0][3] = halves(v.y, v.w, HIGH);
+    } else {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f), w = v;
+        if (has) { v = __ldg((const float4 *)at); w = __ldg((const float4 *)at + 1); }
+        const float m = fmaxf(fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w))),
+                              fmaxf(fmaxf(fabsf(w.x), fabsf(w.y)), fmaxf(fabsf(w.z), fabsf(w.w))));
+        const bool guard = m == INFINITY;
+        uint32_t c[P];
+        const float lo[4] = {v.x, v.y, v.z, v.w}, hi[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            pieces<P>(lo[k], hi[k], guard, c);
+#pragma unroll
+            for (int p = 0; p < P; ++p) b[p][k] = c[p];
+        }
+    }
+}
+
+template <int P, int NT, int GB, bool XS>
 __global__ void __launch_bounds__(THREADS, 1) od_q4_kernel(const Q4Args A)
 {
     extern __shared__ __align__(128) unsigned char smem[];
+    constexpr int IN_BYTES = P == 1 ? 2 : 4;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     const int H = A.H, V = A.V, blocks = H / 32, stages = (blocks + 3) / 4, n_groups = blocks / GB;
     const int n0 = blockIdx.y * (8 * NT);
     const int units = (V + ROWS - 1) / ROWS, step = gridDim.x * WARPS;
-    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (RING * STAGE);
+    unsigned char *const mine = smem + warp * (RING * STAGE);
     const size_t row_bytes = (size_t)H / 2;
 
     // fetching: this lane copies piece lane % 4 of rows lane / 4 and 8 + lane / 4
     int fu = blockIdx.x + warp * gridDim.x, fs = 0, slot_f = 0;
-    const uint32_t put = ring + (lane >> 2) * 64 + ((t ^ ((lane >> 3) & 3)) << 4);
+    const uint32_t put = (uint32_t)__cvta_generic_to_shared(mine) + (lane >> 2) * 64 + ((t ^ ((lane >> 3) & 3)) << 4);
     const uint8_t *f0 = nullptr, *f1 = nullptr;
-    auto aim = [&]() {
-        const int r = fu * ROWS + (lane >> 2);
-        f0 = A.codes + min(r, V - 1) * row_bytes + t * 16;
-        f1 = A.codes + min(r + 8, V - 1) * row_bytes + t * 16;
-    };
     auto fetch = [&]() {
         if (fu < units) {
-            if (fs == 0) aim();
-            if (fs * 4 + t < blocks) {
-                cp16(put + slot_f * STAGE, f0 + (size_t)fs * 64);
-                cp16(put + slot_f * STAGE + 8 * 64, f1 + (size_t)fs * 64);
+            if (fs == 0) {
+                const int r = fu * ROWS + (lane >> 2);
+                f0 = A.codes + min(r, V - 1) * row_bytes + t * 16;
+                f1 = A.codes + min(r + 8, V - 1) * row_bytes + t * 16;
             }
+            if (fs * 4 + t < blocks) {
+                cp16(put + slot_f, f0);
+                cp16(put + slot_f + 8 * 64, f1);
+            }
+            f0 += 64; f1 += 64;
             if (++fs == stages) { fs = 0; fu += step; }
         }
         cp_commit();
-        slot_f = slot_f + 1 == RING ? 0 : slot_f + 1;
+        slot_f = slot_f + STAGE == RING * STAGE ? 0 : slot_f + STAGE;
     };
 #pragma unroll
     for (int i = 0; i < RING - 1; ++i) fetch();
 
-    const uint32_t get = ring + g * 64 + t * 4;
-    const int swz = (g >> 1) & 3;
+    unsigned char *const inputs = smem + WARPS * RING * STAGE;
     const char *x[NT];
     bool has[NT];
+    if constexpr (XS) {
+        // [block of 32 columns][8 tokens][piece][lane]
+        for (int i = threadIdx.x; i < blocks * NT * 32; i += THREADS) {
+            const int n = n0 + (i / 32 % NT) * 8 + g, k = i / 32 / NT * 32 + t * 8;      // (THREADS is a multiple of 32)
+            uint32_t b[P][4];
+            load_inputs<P>((const char *)A.in + ((int64_t)n * A.in_stride + k) * IN_BYTES, n < A.N, b);
 #pragma unroll
-    for (int q = 0; q < NT; ++q) {
-        has[q] = n0 + q * 8 + g < A.N;
-        x[q] = (const char *)A.in + ((int64_t)(has[q] ? n0 + q * 8 + g : 0) * A.in_stride + t * 8) * (P == 1 ? 2 : 4);
+            for (int p = 0; p < P; ++p) ((uint4 *)inputs)[(i / 32 * P + p) * 32 + lane] = make_uint4(b[p][0], b[p][1], b[p][2], b[p][3]);
+        }
+    } else {
+#pragma unroll
+        for (int q = 0; q < NT; ++q) {
+            has[q] = n0 + q * 8 + g < A.N;
+            x[q] = (const char *)A.in + ((int64_t)(has[q] ? n0 + q * 8 + g : 0) * A.in_stride + t * 8) * IN_BYTES;
+        }
     }
+
+    const unsigned char *const get = mine + g * 64 + t * 4;
+    const int swz = (g >> 1) & 3;
+    const int at[4] = {swz << 4, (1 ^ swz) << 4, (2 ^ swz) << 4, (3 ^ swz) << 4};
     int slot = 0;
-    Scales<GB> s0, s1, next0, next1;
-    auto load_scales = [&](int u, int s) {
-        const int r = u * ROWS + g, i = s * (4 / GB);
-        next0.load(A.scales + (size_t)min(r, V - 1) * n_groups + i, n_groups - i, A.wide_scales);
-        next1.load(A.scales + (size_t)min(r + 8, V - 1) * n_groups + i, n_groups - i, A.wide_scales);
+    Scales<GB> next0, next1;
+    const unsigned short *e0, *e1;                         // the next stage's scales
+    auto aim_scales = [&](int u) {
+        const int r = u * ROWS + g;
+        e0 = A.scales + (size_t)min(r, V - 1) * n_groups;
+        e1 = A.scales + (size_t)min(r + 8, V - 1) * n_groups;
+    };
+    auto load_scales = [&](int s) {
+        next0.load(e0, n_groups - s * (4 / GB), A.wide_scales);
+        next1.load(e1, n_groups - s * (4 / GB), A.wide_scales);
+        e0 += 4 / GB; e1 += 4 / GB;
     };
     int u = blockIdx.x + warp * gridDim.x;
-    if (u < units) load_scales(u, 0);
+    if (u < units) { aim_scales(u); load_scales(0); }
+    if (XS) __syncthreads();
     for (; u < units; u += step) {
-        float total[NT][4] = {}, sum[NT][4];
+        float total[NT][4] = {};
+        const uint4 *xs = (const uint4 *)inputs + lane;
         for (int s = 0; s < stages; ++s) {
-            s0 = next0; s1 = next1;
-            if (s + 1 < stages) load_scales(u, s + 1);
-            else if (u + step < units) load_scales(u + step, 0);
+            const Scales<GB> s0 = next0, s1 = next1;
+            if (s + 1 < stages) load_scales(s + 1);
+            else if (u + step < units) { aim_scales(u + step); load_scales(0); }
             cp_wait<RING - 2>();
             __syncwarp();
             fetch();
-            const int here = min(4, blocks - s * 4);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (j >= here) break;
-                uint32_t b[NT][4][P];
+            const unsigned char *const words = get + slot;
+            float sum[NT][4];
+            auto block = [&](int j) {
+                uint32_t b[NT][P][4];
 #pragma unroll
                 for (int q = 0; q < NT; ++q) {
-                    const char *at = x[q] + (size_t)(s * 4 + j) * 32 * (P == 1 ? 2 : 4);
-                    if constexpr (P == 1) {
-                        uint4 v = make_uint4(0, 0, 0, 0);
-                        if (has[q]) v = __ldg((const uint4 *)at);
-                        b[q][0][0] = halves(v.x, v.z, LOW); b[q][1][0] = halves(v.x, v.z, HIGH);
-                        b[q][2][0] = halves(v.y, v.w, LOW); b[q][3][0] = halves(v.y, v.w, HIGH);
+                    if constexpr (XS) {
+#pragma unroll
+                        for (int p = 0; p < P; ++p) {
+                            const uint4 v = xs[((j * NT + q) * P + p) * 32];
+                            b[q][p][0] = v.x; b[q][p][1] = v.y; b[q][p][2] = v.z; b[q][p][3] = v.w;
+                        }
                     } else {
-                        float4 v = make_float4(0.f, 0.f, 0.f, 0.f), w = v;
-                        if (has[q]) { v = __ldg((const float4 *)at); w = __ldg((const float4 *)at + 1); }
-                        const float m = fmaxf(fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w))),
-                                              fmaxf(fmaxf(fabsf(w.x), fabsf(w.y)), fmaxf(fabsf(w.z), fabsf(w.w))));
-                        const bool guard = __any_sync(0xFFFFFFFFu, m == INFINITY);
-                        pieces<P>(v.x, w.x, guard, b[q][0]); pieces<P>(v.y, w.y, guard, b[q][1]);
-                        pieces<P>(v.z, w.z, guard, b[q][2]); pieces<P>(v.w, w.w, guard, b[q][3]);
+                        load_inputs<P>(x[q] + (size_t)(s * 4 + j) * 32 * IN_BYTES, has[q], b[q]);
                     }
                 }
-                const uint32_t at = get + slot * STAGE + ((j ^ swz) << 4);
-                const uint32_t w0 = lds32(at), w1 = lds32(at + 8 * 64);
+                const uint32_t w0 = *(const uint32_t *)(words + at[j]), w1 = *(const uint32_t *)(words + at[j] + 8 * 64);
                 const uint32_t a0[4] = {unpack<0>(w0), unpack<0>(w1), unpack<1>(w0), unpack<1>(w1)};
                 const uint32_t a1[4] = {unpack<2>(w0), unpack<2>(w1), unpack<3>(w0), unpack<3>(w1)};
 #pragma unroll
@@ -241,17 +284,26 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_kernel(const Q4Args A)
                     if (j % GB == 0) sum[q][0] = sum[q][1] = sum[q][2] = sum[q][3] = 0.f;
 #pragma unroll
                     for (int p = 0; p < P; ++p) {
-                        mma(sum[q], a0, b[q][0][p], b[q][1][p]);
-                        mma(sum[q], a1, b[q][2][p], b[q][3][p]);
+                        mma(sum[q], a0, b[q][p][0], b[q][p][1]);
+                        mma(sum[q], a1, b[q][p][2], b[q][p][3]);
                     }
                     if (j % GB == GB - 1) {
-                        const float e0 = s0.get(j / GB), e1 = s1.get(j / GB);
-                        total[q][0] = fmaf(e0, sum[q][0], total[q][0]); total[q][1] = fmaf(e0, sum[q][1], total[q][1]);
-                        total[q][2] = fmaf(e1, sum[q][2], total[q][2]); total[q][3] = fmaf(e1, sum[q][3], total[q][3]);
+                        const float c0 = s0.get(j / GB), c1 = s1.get(j / GB);
+                        total[q][0] = fmaf(c0, sum[q][0], total[q][0]); total[q][1] = fmaf(c0, sum[q][1], total[q][1]);
+                        total[q][2] = fmaf(c1, sum[q][2], total[q][2]); total[q][3] = fmaf(c1, sum[q][3], total[q][3]);
                     }
                 }
+            };
+            if (GB == 4 || s * 4 + 4 <= blocks) {          // (a group of 128 is a whole stage)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) block(j);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 3; ++j)
+                    if (s * 4 + j < blocks) block(j);
             }
-            slot = slot + 1 == RING ? 0 : slot + 1;
+            xs += 4 * NT * P * 32;
+            slot = slot + STAGE == RING * STAGE ? 0 : slot + STAGE;
         }
 #pragma unroll
         for (int q = 0; q < NT; ++q)
@@ -432,13 +484,18 @@ template <int NT> constexpr int grad_bytes = WARPS * 8 * NT * COLS * 4 > ring_by
 typedef void (*Kernel)(Q4Args);
 struct Variant { Kernel kernel; int smem, tokens; };
 
-// by log2(group / 32); forward: tokens of a block by 8, 16, 32 (fp32 inputs: 8), backward: by 8, 16
+// Forward: 8, 16 or 32 tokens to a block, the most (and no more than there are) whose inputs fit into shared memory
+// beside the rings; where those of 8 do not, they stay in global memory. Backward: 8 or 16.
+constexpr int IN_SMEM = 227 * 1024 - ring_bytes;
+template <int P, int NT, int GB>
+Variant in_smem(int32_t H) { return {od_q4_kernel<P, NT, GB, true>, ring_bytes + H * 16 * NT * P, 8 * NT}; }
 template <int GB>
-Variant forward_of(bool f32, int N)
+Variant forward_of(bool f32, int N, int32_t H)
 {
-    if (f32) return {od_q4_kernel<3, 1, GB>, ring_bytes, 8};
-    if (N <= 8) return {od_q4_kernel<1, 1, GB>, ring_bytes, 8};
-    return N <= 16 ? Variant{od_q4_kernel<1, 2, GB>, ring_bytes, 16} : Variant{od_q4_kernel<1, 4, GB>, ring_bytes, 32};
+    if (f32) return H <= IN_SMEM / 48 ? in_smem<3, 1, GB>(H) : Variant{od_q4_kernel<3, 1, GB, false>, ring_bytes, 8};
+    if (N > 16 && H <= IN_SMEM / 64) return in_smem<1, 4, GB>(H);
+    if (N > 8 && H <= IN_SMEM / 32) return in_smem<1, 2, GB>(H);
+    return H <= IN_SMEM / 16 ? in_smem<1, 1, GB>(H) : Variant{od_q4_kernel<1, 1, GB, false>, ring_bytes, 8};
 }
 template <int GB>
 Variant backward_of(bool f32, int N)
@@ -446,10 +503,10 @@ Variant backward_of(bool f32, int N)
     if (f32) return N <= 8 ? Variant{od_q4_grad_kernel<3, 1, GB>, grad_bytes<1>, 8} : Variant{od_q4_grad_kernel<3, 2, GB>, grad_bytes<2>, 16};
     return N <= 8 ? Variant{od_q4_grad_kernel<2, 1, GB>, grad_bytes<1>, 8} : Variant{od_q4_grad_kernel<2, 2, GB>, grad_bytes<2>, 16};
 }
-Variant variant(bool backward, int32_t G, bool f32, int N)
+Variant variant(bool backward, int32_t G, bool f32, int N, int32_t H)
 {
     if (backward) return G == 32 ? backward_of<1>(f32, N) : G == 64 ? backward_of<2>(f32, N) : backward_of<4>(f32, N);
-    return G == 32 ? forward_of<1>(f32, N) : G == 64 ? forward_of<2>(f32, N) : forward_of<4>(f32, N);
+    return G == 32 ? forward_of<1>(f32, N, H) : G == 64 ? forward_of<2>(f32, N, H) : forward_of<4>(f32, N, H);
 }
 
 void configure(cudaLaunchConfig_t &cfg, cudaLaunchAttribute (&attr)[2], const Variant &v, unsigned blocks, unsigned tiles, unsigned cluster)
@@ -472,9 +529,9 @@ cudaError_t od_q4_prepare_device(int32_t (*clusters)[OD_Q4_MAX_SPLIT + 1])
     for (int backward = 0; backward < 2; ++backward)
         for (int32_t G = 32; G <= 128; G *= 2)
             for (int f32 = 0; f32 < 2; ++f32)
-                for (int N = 8; N <= 32; N *= 2) {
-                    const Variant v = variant(backward, G, f32, N);
-                    cudaError_t e = cudaFuncSetAttribute((const void *)v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, v.smem);
+                for (int N = 8; N <= 64; N *= 2) {         // (64: none in shared memory)
+                    const Variant v = variant(backward, G, f32, N, N == 64 ? 65536 : 128);
+                    cudaError_t e = cudaFuncSetAttribute((const void *)v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
                     if (e == cudaSuccess && backward) e = cudaFuncSetAttribute((const void *)v.kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
                     if (e != cudaSuccess) return e;
                 }
@@ -482,7 +539,7 @@ cudaError_t od_q4_prepare_device(int32_t (*clusters)[OD_Q4_MAX_SPLIT + 1])
         for (int n = 1; n <= MAX_SPLIT; ++n) {
             cudaLaunchConfig_t cfg;
             cudaLaunchAttribute attr[2];
-            const Variant v = variant(true, 32, true, wide ? 16 : 8);
+            const Variant v = variant(true, 32, true, wide ? 16 : 8, 128);
             configure(cfg, attr, v, (unsigned)n, 1, (unsigned)n);
             int here = 0;
             if (cudaOccupancyMaxActiveClusters(&here, (const void *)v.kernel, &cfg) != cudaSuccess) {
@@ -497,7 +554,7 @@ cudaError_t od_q4_prepare_device(int32_t (*clusters)[OD_Q4_MAX_SPLIT + 1])
 cudaError_t od_launch_q4(const od_ctx *c, bool backward, int32_t N, int32_t V, int32_t H, int32_t G, const void *a, int32_t a_dtype,
                          int64_t as, const void *codes, const void *scales, void *b, int32_t b_dtype, int64_t bs, cudaStream_t s)
 {
-    const Variant v = variant(backward, G, a_dtype == OD_F32, N);
+    const Variant v = variant(backward, G, a_dtype == OD_F32, N, H);
     Q4Args args = {a, as, (const uint8_t *)codes, (const unsigned short *)scales, b, bs, N, V, H, a_dtype == OD_F32, b_dtype == OD_F32,
                    H % COLS == 0 && ((uintptr_t)scales & 7u) == 0, 1, 1};
     unsigned blocks;
