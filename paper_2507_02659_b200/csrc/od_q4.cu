@@ -26,6 +26,9 @@ constexpr int ROWS = 16;                                   // of a stage, and of
 constexpr int COLS = 128;                                  // of a stage: four blocks of 32
 constexpr int STAGE = ROWS * COLS / 2;                     // bytes
 constexpr int RING = 6;                                    // stages of a warp
+constexpr int WIDE = 8;                                    // forward: blocks of 32 columns to a stage
+constexpr int WIDE_STAGE = ROWS * WIDE * 16;
+constexpr int WIDE_RING = 3;
 constexpr int MAX_SPLIT = OD_Q4_MAX_SPLIT;                 // blocks that share the rows of a gradient (a cluster)
 
 struct Q4Args {
@@ -180,16 +183,17 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_kernel(const Q4Args A)
     constexpr int IN_BYTES = P == 1 ? 2 : 4;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-    const int H = A.H, V = A.V, blocks = H / 32, stages = (blocks + 3) / 4, n_groups = blocks / GB;
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0);    // (known to be the same in the warp's lanes)
+    const int H = A.H, V = A.V, blocks = H / 32, stages = (blocks + WIDE - 1) / WIDE, n_groups = blocks / GB;
     const int n0 = blockIdx.y * (8 * NT);
     const int units = (V + ROWS - 1) / ROWS, step = gridDim.x * WARPS;
-    unsigned char *const mine = smem + warp * (RING * STAGE);
+    unsigned char *const mine = smem + warp * (WIDE_RING * WIDE_STAGE);
     const size_t row_bytes = (size_t)H / 2;
 
-    // fetching: this lane copies piece lane % 4 of rows lane / 4 and 8 + lane / 4
+    // fetching: this lane copies pieces lane % 4 and 4 + lane % 4 of rows lane / 4 and 8 + lane / 4
     int fu = blockIdx.x + warp * gridDim.x, fs = 0, slot_f = 0;
-    const uint32_t put = (uint32_t)__cvta_generic_to_shared(mine) + (lane >> 2) * 64 + ((t ^ ((lane >> 3) & 3)) << 4);
+    const uint32_t put = (uint32_t)__cvta_generic_to_shared(mine) + (lane >> 2) * 128 + ((t ^ (lane >> 2)) << 4);
     const uint8_t *f0 = nullptr, *f1 = nullptr;
     auto fetch = [&]() {
         if (fu < units) {
@@ -198,20 +202,19 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_kernel(const Q4Args A)
                 f0 = A.codes + min(r, V - 1) * row_bytes + t * 16;
                 f1 = A.codes + min(r + 8, V - 1) * row_bytes + t * 16;
             }
-            if (fs * 4 + t < blocks) {
-                cp16(put + slot_f, f0);
-                cp16(put + slot_f + 8 * 64, f1);
-            }
-            f0 += 64; f1 += 64;
+            const uint32_t to = put + slot_f;
+            if (fs * WIDE + t < blocks) { cp16(to, f0); cp16(to + 8 * 128, f1); }
+            if (fs * WIDE + 4 + t < blocks) { cp16(to ^ 64, f0 + 64); cp16((to ^ 64) + 8 * 128, f1 + 64); }
+            f0 += 16 * WIDE; f1 += 16 * WIDE;
             if (++fs == stages) { fs = 0; fu += step; }
         }
         cp_commit();
-        slot_f = slot_f + STAGE == RING * STAGE ? 0 : slot_f + STAGE;
+        slot_f = slot_f + WIDE_STAGE == WIDE_RING * WIDE_STAGE ? 0 : slot_f + WIDE_STAGE;
     };
 #pragma unroll
-    for (int i = 0; i < RING - 1; ++i) fetch();
+    for (int i = 0; i < WIDE_RING - 1; ++i) fetch();
 
-    unsigned char *const inputs = smem + WARPS * RING * STAGE;
+    unsigned char *const inputs = smem + WARPS * WIDE_RING * WIDE_STAGE;
     const char *x[NT];
     bool has[NT];
     if constexpr (XS) {
@@ -231,11 +234,11 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_kernel(const Q4Args A)
         }
     }
 
-    const unsigned char *const get = mine + g * 64 + t * 4;
-    const int swz = (g >> 1) & 3;
-    const int at[4] = {swz << 4, (1 ^ swz) << 4, (2 ^ swz) << 4, (3 ^ swz) << 4};
+    const unsigned char *at[WIDE];                          // this lane's words of the first slot
+#pragma unroll
+    for (int j = 0; j < WIDE; ++j) at[j] = mine + g * 128 + ((j ^ g) << 4) + t * 4;
     int slot = 0;
-    Scales<GB> next0, next1;
+    Scales<GB> next0[2], next1[2];
     const unsigned short *e0, *e1;                         // the next stage's scales
     auto aim_scales = [&](int u) {
         const int r = u * ROWS + g;
@@ -243,9 +246,15 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_kernel(const Q4Args A)
         e1 = A.scales + (size_t)min(r + 8, V - 1) * n_groups;
     };
     auto load_scales = [&](int s) {
-        next0.load(e0, n_groups - s * (4 / GB), A.wide_scales);
-        next1.load(e1, n_groups - s * (4 / GB), A.wide_scales);
-        e0 += 4 / GB; e1 += 4 / GB;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int left = n_groups - (s * WIDE + 4 * i) / GB;
+            if (i == 0 || left > 0) {
+                next0[i].load(e0 + 4 / GB * i, left, A.wide_scales);
+                next1[i].load(e1 + 4 / GB * i, left, A.wide_scales);
+            }
+        }
+        e0 += WIDE / GB; e1 += WIDE / GB;
     };
     int u = blockIdx.x + warp * gridDim.x;
     if (u < units) { aim_scales(u); load_scales(0); }
@@ -254,13 +263,12 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_kernel(const Q4Args A)
         float total[NT][4] = {};
         const uint4 *xs = (const uint4 *)inputs + lane;
         for (int s = 0; s < stages; ++s) {
-            const Scales<GB> s0 = next0, s1 = next1;
+            const Scales<GB> s0[2] = {next0[0], next0[1]}, s1[2] = {next1[0], next1[1]};
             if (s + 1 < stages) load_scales(s + 1);
             else if (u + step < units) { aim_scales(u + step); load_scales(0); }
-            cp_wait<RING - 2>();
+            cp_wait<WIDE_RING - 2>();
             __syncwarp();
             fetch();
-            const unsigned char *const words = get + slot;
             float sum[NT][4];
             auto block = [&](int j) {
                 uint32_t b[NT][P][4];
@@ -273,10 +281,10 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_kernel(const Q4Args A)
                             b[q][p][0] = v.x; b[q][p][1] = v.y; b[q][p][2] = v.z; b[q][p][3] = v.w;
                         }
                     } else {
-                        load_inputs<P>(x[q] + (size_t)(s * 4 + j) * 32 * IN_BYTES, has[q], b[q]);
+                        load_inputs<P>(x[q] + (size_t)(s * WIDE + j) * 32 * IN_BYTES, has[q], b[q]);
                     }
                 }
-                const uint32_t w0 = *(const uint32_t *)(words + at[j]), w1 = *(const uint32_t *)(words + at[j] + 8 * 64);
+                const uint32_t w0 = *(const uint32_t *)(at[j] + slot), w1 = *(const uint32_t *)(at[j] + slot + 8 * 128);
                 const uint32_t a0[4] = {unpack<0>(w0), unpack<0>(w1), unpack<1>(w0), unpack<1>(w1)};
                 const uint32_t a1[4] = {unpack<2>(w0), unpack<2>(w1), unpack<3>(w0), unpack<3>(w1)};
 #pragma unroll
@@ -288,22 +296,22 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_kernel(const Q4Args A)
                         mma(sum[q], a1, b[q][p][2], b[q][p][3]);
                     }
                     if (j % GB == GB - 1) {
-                        const float c0 = s0.get(j / GB), c1 = s1.get(j / GB);
+                        const float c0 = s0[j / 4].get(j % 4 / GB), c1 = s1[j / 4].get(j % 4 / GB);
                         total[q][0] = fmaf(c0, sum[q][0], total[q][0]); total[q][1] = fmaf(c0, sum[q][1], total[q][1]);
                         total[q][2] = fmaf(c1, sum[q][2], total[q][2]); total[q][3] = fmaf(c1, sum[q][3], total[q][3]);
                     }
                 }
             };
-            if (GB == 4 || s * 4 + 4 <= blocks) {          // (a group of 128 is a whole stage)
+            if (s * WIDE + WIDE <= blocks) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) block(j);
+                for (int j = 0; j < WIDE; ++j) block(j);
             } else {
 #pragma unroll
-                for (int j = 0; j < 3; ++j)
-                    if (s * 4 + j < blocks) block(j);
+                for (int j = 0; j < WIDE - 1; ++j)
+                    if (s * WIDE + j < blocks) block(j);
             }
-            xs += 4 * NT * P * 32;
-            slot = slot + STAGE == RING * STAGE ? 0 : slot + STAGE;
+            xs += WIDE * NT * P * 32;
+            slot = slot + WIDE_STAGE == WIDE_RING * WIDE_STAGE ? 0 : slot + WIDE_STAGE;
         }
 #pragma unroll
         for (int q = 0; q < NT; ++q)
@@ -478,7 +486,7 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
     if (split > 1) { od_cluster_arrive(); od_cluster_wait(); }
 }
 
-constexpr int ring_bytes = WARPS * RING * STAGE;
+constexpr int ring_bytes = WARPS * RING * STAGE, wide_bytes = WARPS * WIDE_RING * WIDE_STAGE;
 template <int NT> constexpr int grad_bytes = WARPS * 8 * NT * COLS * 4 > ring_bytes ? WARPS * 8 * NT * COLS * 4 : ring_bytes;
 
 typedef void (*Kernel)(Q4Args);
@@ -486,16 +494,16 @@ struct Variant { Kernel kernel; int smem, tokens; };
 
 // Forward: 8, 16 or 32 tokens to a block, the most (and no more than there are) whose inputs fit into shared memory
 // beside the rings; where those of 8 do not, they stay in global memory. Backward: 8 or 16.
-constexpr int IN_SMEM = 227 * 1024 - ring_bytes;
+constexpr int IN_SMEM = 227 * 1024 - wide_bytes;
 template <int P, int NT, int GB>
-Variant in_smem(int32_t H) { return {od_q4_kernel<P, NT, GB, true>, ring_bytes + H * 16 * NT * P, 8 * NT}; }
+Variant in_smem(int32_t H) { return {od_q4_kernel<P, NT, GB, true>, wide_bytes + H * 16 * NT * P, 8 * NT}; }
 template <int GB>
 Variant forward_of(bool f32, int N, int32_t H)
 {
-    if (f32) return H <= IN_SMEM / 48 ? in_smem<3, 1, GB>(H) : Variant{od_q4_kernel<3, 1, GB, false>, ring_bytes, 8};
+    if (f32) return H <= IN_SMEM / 48 ? in_smem<3, 1, GB>(H) : Variant{od_q4_kernel<3, 1, GB, false>, wide_bytes, 8};
     if (N > 16 && H <= IN_SMEM / 64) return in_smem<1, 4, GB>(H);
     if (N > 8 && H <= IN_SMEM / 32) return in_smem<1, 2, GB>(H);
-    return H <= IN_SMEM / 16 ? in_smem<1, 1, GB>(H) : Variant{od_q4_kernel<1, 1, GB, false>, ring_bytes, 8};
+    return H <= IN_SMEM / 16 ? in_smem<1, 1, GB>(H) : Variant{od_q4_kernel<1, 1, GB, false>, wide_bytes, 8};
 }
 template <int GB>
 Variant backward_of(bool f32, int N)
