@@ -40,6 +40,7 @@ struct Q4Args {
     int64_t out_stride;
     int32_t N, V, H, in_f32, out_f32;
     int32_t wide_scales;                                   // the scales of a stage's row are one aligned word
+    uint32_t bf16_128;                                     // see unpack
     int32_t split, col_warps;                              // backward: blocks of a cluster, warps side by side
 };
 
@@ -55,6 +56,12 @@ __device__ __forceinline__ uint32_t lds32(uint32_t at)
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
     return v;
 }
+__device__ __forceinline__ uint4 lds128(uint32_t at)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
 __device__ __forceinline__ float lds_cluster(uint32_t at)
 {
     float v;
@@ -67,11 +74,14 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// codes i and i + 4 of a word, less 8, as a pair of bf16: 128 + u has u in its last bits
+// codes i and i + 4 of a word, less 8, as a pair of bf16: 128 + u has u in its last bits. (bf16_128, a pair of 128, is an
+// argument of the kernel: a mask and an or with two constants that the compiler knows are two instructions, and with one
+// in a register they are one.)
 template <int I>
-__device__ __forceinline__ uint32_t unpack(uint32_t w)
+__device__ __forceinline__ uint32_t unpack(uint32_t w, uint32_t bf16_128)
 {
-    uint32_t m = ((w >> 4 * I) & 0x000F000Fu) | 0x43004300u, d;
+    uint32_t m, d;
+    asm("lop3.b32 %0, %1, 0x000F000F, %2, 0xEA;" : "=r"(m) : "r"(w >> 4 * I), "r"(bf16_128));
     asm("sub.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(m), "r"(0x43084308u));
     return d;
 }
@@ -234,9 +244,7 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_kernel(const Q4Args A)
         }
     }
 
-    const unsigned char *at[WIDE];                          // this lane's words of the first slot
-#pragma unroll
-    for (int j = 0; j < WIDE; ++j) at[j] = mine + g * 128 + ((j ^ g) << 4) + t * 4;
+    const uint32_t get = (uint32_t)__cvta_generic_to_shared(mine) + g * 128 + (g << 4) + t * 4;   // this lane's first word of the first slot
     int slot = 0;
     Scales<GB> next0[2], next1[2];
     const unsigned short *e0, *e1;                         // the next stage's scales
@@ -261,7 +269,7 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_kernel(const Q4Args A)
     if (XS) __syncthreads();
     for (; u < units; u += step) {
         float total[NT][4] = {};
-        const uint4 *xs = (const uint4 *)inputs + lane;
+        uint32_t xs = (uint32_t)__cvta_generic_to_shared(inputs) + lane * 16;
         for (int s = 0; s < stages; ++s) {
             const Scales<GB> s0[2] = {next0[0], next0[1]}, s1[2] = {next1[0], next1[1]};
             if (s + 1 < stages) load_scales(s + 1);
@@ -277,16 +285,16 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_kernel(const Q4Args A)
                     if constexpr (XS) {
 #pragma unroll
                         for (int p = 0; p < P; ++p) {
-                            const uint4 v = xs[((j * NT + q) * P + p) * 32];
+                            const uint4 v = lds128(xs + ((j * NT + q) * P + p) * 512);
                             b[q][p][0] = v.x; b[q][p][1] = v.y; b[q][p][2] = v.z; b[q][p][3] = v.w;
                         }
                     } else {
                         load_inputs<P>(x[q] + (size_t)(s * WIDE + j) * 32 * IN_BYTES, has[q], b[q]);
                     }
                 }
-                const uint32_t w0 = *(const uint32_t *)(at[j] + slot), w1 = *(const uint32_t *)(at[j] + slot + 8 * 128);
-                const uint32_t a0[4] = {unpack<0>(w0), unpack<0>(w1), unpack<1>(w0), unpack<1>(w1)};
-                const uint32_t a1[4] = {unpack<2>(w0), unpack<2>(w1), unpack<3>(w0), unpack<3>(w1)};
+                const uint32_t w0 = lds32((get + slot) ^ (j << 4)), w1 = lds32(((get + slot) ^ (j << 4)) + 8 * 128);
+                const uint32_t a0[4] = {unpack<0>(w0, A.bf16_128), unpack<0>(w1, A.bf16_128), unpack<1>(w0, A.bf16_128), unpack<1>(w1, A.bf16_128)};
+                const uint32_t a1[4] = {unpack<2>(w0, A.bf16_128), unpack<2>(w1, A.bf16_128), unpack<3>(w0, A.bf16_128), unpack<3>(w1, A.bf16_128)};
 #pragma unroll
                 for (int q = 0; q < NT; ++q) {
                     if (j % GB == 0) sum[q][0] = sum[q][1] = sum[q][2] = sum[q][3] = 0.f;
@@ -310,7 +318,7 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_kernel(const Q4Args A)
                 for (int j = 0; j < WIDE - 1; ++j)
                     if (s * WIDE + j < blocks) block(j);
             }
-            xs += WIDE * NT * P * 32;
+            xs += WIDE * NT * P * 512;
             slot = slot + WIDE_STAGE == WIDE_RING * WIDE_STAGE ? 0 : slot + WIDE_STAGE;
         }
 #pragma unroll
@@ -439,8 +447,8 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
             }
             const uint32_t at = get + slot * STAGE + ((j ^ t) << 4);
             const uint32_t w01 = halves(lds32(at), lds32(at + 64), pick), w23 = halves(lds32(at + 128), lds32(at + 192), pick);
-            const uint32_t a0[4] = {unpack<0>(w01), unpack<1>(w01), unpack<0>(w23), unpack<1>(w23)};
-            const uint32_t a1[4] = {unpack<2>(w01), unpack<3>(w01), unpack<2>(w23), unpack<3>(w23)};
+            const uint32_t a0[4] = {unpack<0>(w01, A.bf16_128), unpack<1>(w01, A.bf16_128), unpack<0>(w23, A.bf16_128), unpack<1>(w23, A.bf16_128)};
+            const uint32_t a1[4] = {unpack<2>(w01, A.bf16_128), unpack<3>(w01, A.bf16_128), unpack<2>(w23, A.bf16_128), unpack<3>(w23, A.bf16_128)};
 #pragma unroll
             for (int q = 0; q < NT; ++q)
 #pragma unroll
@@ -564,7 +572,7 @@ cudaError_t od_launch_q4(const od_ctx *c, bool backward, int32_t N, int32_t V, i
 {
     const Variant v = variant(backward, G, a_dtype == OD_F32, N, H);
     Q4Args args = {a, as, (const uint8_t *)codes, (const unsigned short *)scales, b, bs, N, V, H, a_dtype == OD_F32, b_dtype == OD_F32,
-                   H % COLS == 0 && ((uintptr_t)scales & 7u) == 0, 1, 1};
+                   H % COLS == 0 && ((uintptr_t)scales & 7u) == 0, 0x43004300u, 1, 1};
     unsigned blocks;
     if (!backward) {
         const int64_t units = ((int64_t)V + ROWS - 1) / ROWS;
