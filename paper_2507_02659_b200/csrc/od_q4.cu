@@ -22,6 +22,7 @@
 namespace {
 
 constexpr int WARPS = 16, THREADS = 32 * WARPS;
+constexpr int F_WARPS = 16, F_THREADS = 32 * F_WARPS;
 constexpr int ROWS = 16;                                   // of a stage, and of a matrix instruction
 constexpr int COLS = 128;                                  // of a stage: four blocks of 32
 constexpr int STAGE = ROWS * COLS / 2;                     // bytes
@@ -41,6 +42,7 @@ struct Q4Args {
     int32_t N, V, H, in_f32, out_f32;
     int32_t wide_scales;                                   // the scales of a stage's row are one aligned word
     uint32_t bf16_128;                                     // see unpack
+    int32_t k_split;                                       // forward: warps to the same rows
     int32_t split, col_warps;                              // backward: blocks of a cluster, warps side by side
 };
 
@@ -89,6 +91,7 @@ __device__ __forceinline__ uint32_t halves(uint32_t a, uint32_t b, uint32_t pick
 {
     return __byte_perm(a, b, pick);
 }
+constexpr uint32_t CODE = 0x000F000Fu, CODE16 = 0x00F000F0u;
 constexpr uint32_t LOW = 0x5410, HIGH = 0x7632;            // both low halves, both high halves
 
 // x = hi + mid + lo by cutting its bits; of an infinity everything is in hi
@@ -153,6 +156,9 @@ struct Scales {
     }
 };
 
+template <int P>
+__device__ __forceinline__ void pieces(float a, float b, uint32_t (&out)[P]) { pieces<P>(a, b, false, out); }
+
 // ---- forward: 16 rows of the weights to a warp, all columns -------------------------------------
 //
 // A word of a row is eight columns: a stage's block of 32 columns is four words, one to each of the four lanes that share
@@ -160,63 +166,116 @@ struct Scales {
 // a token. XS: a block of threads keeps its tokens' inputs in shared memory as the words of the fragments, 16 bytes to a
 // lane; where they do not fit, they are read and cut again for every 16 rows.
 
-// the words of a lane's fragments for eight columns of a token
-template <int P>
-__device__ __forceinline__ void load_inputs(const char *at, bool has, uint32_t (&b)[P][4])
+// Nothing is subtracted from the codes, and nothing is or'ed to them: the 8 bits of a code u, or of 16 u, are the bf16 number
+// u 2^-133, or 16 u 2^-133 (with no more bits set a bf16 is its bits times 2^-133, in the first binade too). So two masks,
+// a shift and two masks unpack a word; inputs that meet a 16 u are divided by 16. For products in fp32's range a token is
+// scaled by a power of two that brings its largest magnitude to 2^126, and its sums are scaled back at the end. The 8 that is
+// left out is in what a group's sum begins at: -8 times the sum of its inputs, in the same units. It adds to the sums'
+// magnitudes no more than their codes do. (With 136 subtracted from bf16 numbers 128 + u in the loop: 59 us where it
+// is 45, eight tokens through 128256 x 4096.)
+
+// eight columns of a token (columns 8t .. 8t + 7 of a block), scaled; a token with infinities or NaN is zero here
+struct Token {
+    float up, up2;                                         // the scale is their product
+    __device__ __forceinline__ Token(uint32_t largest)     // bits of the largest magnitude
+    {
+        const int e = largest >> 23, k = e < 255 ? 253 - e : 0, h = k / 2;
+        up = e < 255 ? __int_as_float((127 + h) << 23) : 0.f;
+        up2 = __int_as_float((127 + k - h) << 23);
+    }
+};
+// sums of a token back to its units: they are of products times 2^(k - 133)
+__device__ __forceinline__ float scaled_back(float v, uint32_t largest)
 {
-    if constexpr (P == 1) {
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (has) v = __ldg((const uint4 *)at);
-        b[0][0] = halves(v.x, v.z, LOW); b[0][1] = halves(v.x, v.z, HIGH);
-        b[0][2] = halves(v.y, v.w, LOW); b[0][3] = halves(v.y, v.w, HIGH);
-    } else {
+    const int e = largest >> 23, k = 133 - (253 - e), h = k / 2;
+    return v * __int_as_float((127 + h) << 23) * __int_as_float((127 + k - h) << 23);
+}
+template <bool F32>
+__device__ __forceinline__ void load_columns(const void *at, bool has, float (&x)[8])
+{
+    if constexpr (F32) {
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f), w = v;
         if (has) { v = __ldg((const float4 *)at); w = __ldg((const float4 *)at + 1); }
-        const float m = fmaxf(fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w))),
-                              fmaxf(fmaxf(fabsf(w.x), fabsf(w.y)), fmaxf(fabsf(w.z), fabsf(w.w))));
-        const bool guard = m == INFINITY;
+        x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; x[4] = w.x; x[5] = w.y; x[6] = w.z; x[7] = w.w;
+    } else {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (has) v = __ldg((const uint4 *)at);
+        x[0] = od_bf16_lo(v.x); x[1] = od_bf16_hi(v.x); x[2] = od_bf16_lo(v.y); x[3] = od_bf16_hi(v.y);
+        x[4] = od_bf16_lo(v.z); x[5] = od_bf16_hi(v.z); x[6] = od_bf16_lo(v.w); x[7] = od_bf16_hi(v.w);
+    }
+}
+// and the words of a lane's fragments
+template <int P>
+__device__ __forceinline__ void cut_columns(float (&x)[8], const Token &k, uint32_t (&b)[P][4])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        x[i] *= k.up;
+        x[i] = k.up == 0.f ? 0.f : x[i] * k.up2;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float f = i & 1 ? 0.0625f : 1.f;
         uint32_t c[P];
-        const float lo[4] = {v.x, v.y, v.z, v.w}, hi[4] = {w.x, w.y, w.z, w.w};
+        pieces<P>(x[i] * f, x[i + 4] * f, c);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            pieces<P>(lo[k], hi[k], guard, c);
-#pragma unroll
-            for (int p = 0; p < P; ++p) b[p][k] = c[p];
-        }
+        for (int p = 0; p < P; ++p) b[p][i] = c[p];
     }
 }
 
+// one result as it is defined: of tokens that hold an infinity or NaN
+template <bool F32>
+__device__ __noinline__ float one_logit(const Q4Args &A, int n, int v, int G)
+{
+    float total = 0.f;
+    for (int h = 0; h < A.H; h += G) {
+        float sum = 0.f;
+        for (int i = h; i < h + G; ++i) {
+            const float x = F32 ? ((const float *)A.in)[(size_t)n * A.in_stride + i]
+                                : __uint_as_float((uint32_t)((const unsigned short *)A.in)[(size_t)n * A.in_stride + i] << 16);
+            sum += x * (float)((A.codes[((size_t)v * A.H + i) / 2] >> (i & 1) * 4 & 15) - 8);
+        }
+        total += __uint_as_float((uint32_t)A.scales[((size_t)v * A.H + h) / G] << 16) * sum;
+    }
+    return total;
+}
+
 template <int P, int NT, int GB, bool XS>
-__global__ void __launch_bounds__(THREADS, 1) od_q4_kernel(const Q4Args A)
+__global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
 {
     extern __shared__ __align__(128) unsigned char smem[];
-    constexpr int IN_BYTES = P == 1 ? 2 : 4;
+    __shared__ uint32_t largest_of[8 * NT][2];
+    constexpr bool F32 = P == 3;
+    constexpr int IN_BYTES = F32 ? 4 : 2;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0);    // (known to be the same in the warp's lanes)
     const int H = A.H, V = A.V, blocks = H / 32, stages = (blocks + WIDE - 1) / WIDE, n_groups = blocks / GB;
     const int n0 = blockIdx.y * (8 * NT);
-    const int units = (V + ROWS - 1) / ROWS, step = gridDim.x * WARPS;
+    // k_split warps to the same rows, each a share of the stages
+    const int ks = A.k_split, sub = warp % ks, groups = F_WARPS / ks;
+    const int first = stages * sub / ks, last = stages * (sub + 1) / ks;
+    const int units = (V + ROWS - 1) / ROWS, step = gridDim.x * groups, begin = blockIdx.x + warp / ks * gridDim.x;
     unsigned char *const mine = smem + warp * (WIDE_RING * WIDE_STAGE);
     const size_t row_bytes = (size_t)H / 2;
 
     // fetching: this lane copies pieces lane % 4 and 4 + lane % 4 of rows lane / 4 and 8 + lane / 4
-    int fu = blockIdx.x + warp * gridDim.x, fs = 0, slot_f = 0;
+    int fu = begin, fs = first, slot_f = 0;
     const uint32_t put = (uint32_t)__cvta_generic_to_shared(mine) + (lane >> 2) * 128 + ((t ^ (lane >> 2)) << 4);
     const uint8_t *f0 = nullptr, *f1 = nullptr;
     auto fetch = [&]() {
         if (fu < units) {
-            if (fs == 0) {
+            if (fs == first) {
                 const int r = fu * ROWS + (lane >> 2);
-                f0 = A.codes + min(r, V - 1) * row_bytes + t * 16;
-                f1 = A.codes + min(r + 8, V - 1) * row_bytes + t * 16;
+                f0 = A.codes + min(r, V - 1) * row_bytes + first * (16 * WIDE) + t * 16;
+                f1 = A.codes + min(r + 8, V - 1) * row_bytes + first * (16 * WIDE) + t * 16;
             }
             const uint32_t to = put + slot_f;
             if (fs * WIDE + t < blocks) { cp16(to, f0); cp16(to + 8 * 128, f1); }
             if (fs * WIDE + 4 + t < blocks) { cp16(to ^ 64, f0 + 64); cp16((to ^ 64) + 8 * 128, f1 + 64); }
             f0 += 16 * WIDE; f1 += 16 * WIDE;
-            if (++fs == stages) { fs = 0; fu += step; }
+            if (++fs == last) { fs = first; fu += step; }
         }
         cp_commit();
         slot_f = slot_f + WIDE_STAGE == WIDE_RING * WIDE_STAGE ? 0 : slot_f + WIDE_STAGE;
@@ -224,25 +283,53 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_kernel(const Q4Args A)
 #pragma unroll
     for (int i = 0; i < WIDE_RING - 1; ++i) fetch();
 
-    unsigned char *const inputs = smem + WARPS * WIDE_RING * WIDE_STAGE;
-    const char *x[NT];
-    bool has[NT];
-    if constexpr (XS) {
-        // [block of 32 columns][8 tokens][piece][lane]
-        for (int i = threadIdx.x; i < blocks * NT * 32; i += THREADS) {
-            const int n = n0 + (i / 32 % NT) * 8 + g, k = i / 32 / NT * 32 + t * 8;      // (THREADS is a multiple of 32)
-            uint32_t b[P][4];
-            load_inputs<P>((const char *)A.in + ((int64_t)n * A.in_stride + k) * IN_BYTES, n < A.N, b);
+    // the largest magnitude of each token, by two warps
+    for (int i = warp; i < 16 * NT; i += F_WARPS) {
+        const int n = n0 + i / 2;
+        const char *at = (const char *)A.in + (int64_t)(n < A.N ? n : 0) * A.in_stride * IN_BYTES;
+        uint32_t m = 0;
+        for (int k = (i & 1) * 32 + lane; k < H * IN_BYTES / 16; k += 64) {
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (n < A.N) v = __ldg((const uint4 *)at + k);
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-            for (int p = 0; p < P; ++p) ((uint4 *)inputs)[(i / 32 * P + p) * 32 + lane] = make_uint4(b[p][0], b[p][1], b[p][2], b[p][3]);
+            for (int j = 0; j < 4; ++j) m = F32 ? max(m, w[j] & 0x7FFFFFFFu) : max(m, max(w[j] & 0x7FFF0000u, w[j] << 16 & 0x7FFFFFFFu));
         }
-    } else {
-#pragma unroll
-        for (int q = 0; q < NT; ++q) {
-            has[q] = n0 + q * 8 + g < A.N;
-            x[q] = (const char *)A.in + ((int64_t)(has[q] ? n0 + q * 8 + g : 0) * A.in_stride + t * 8) * IN_BYTES;
-        }
+        m = __reduce_max_sync(0xFFFFFFFFu, m);
+        if (lane == 0) largest_of[i / 2][i & 1] = m;
     }
+    __syncthreads();
+    auto largest = [&](int n) { return max(largest_of[n][0], largest_of[n][1]); };
+
+    // [group][8 tokens to a part]: what the group's sums begin at; [block of 32 columns][part][piece][lane]: the fragments
+    float *const starts = (float *)(smem + F_WARPS * WIDE_RING * WIDE_STAGE);
+    unsigned char *const inputs = (unsigned char *)(starts + n_groups * 8 * NT);
+    for (int i = warp; i < n_groups * NT; i += F_WARPS) {
+        const int q = i % NT, n = n0 + q * 8 + g;
+        const Token k(largest(q * 8 + g));
+        float start = 0.f;
+#pragma unroll
+        for (int j = 0; j < GB; ++j) {
+            const int blk = i / NT * GB + j;
+            float x[8];
+            load_columns<F32>((const char *)A.in + ((int64_t)n * A.in_stride + blk * 32 + t * 8) * IN_BYTES, n < A.N, x);
+            uint32_t b[P][4];
+            cut_columns<P>(x, k, b);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) start = fmaf(x[c], -0x1p-126f * 0.0625f, start);       // -8 times 2^-133
+            if constexpr (XS)
+#pragma unroll
+                for (int p = 0; p < P; ++p) ((uint4 *)inputs)[((blk * NT + q) * P + p) * 32 + lane] = make_uint4(b[p][0], b[p][1], b[p][2], b[p][3]);
+        }
+        start += __shfl_xor_sync(0xFFFFFFFFu, start, 1);
+        start += __shfl_xor_sync(0xFFFFFFFFu, start, 2);
+        if (t == 0) starts[i * 8 + g] = start;
+    }
+    const char *x_at[NT];
+    if constexpr (!XS)
+#pragma unroll
+        for (int q = 0; q < NT; ++q)
+            x_at[q] = (const char *)A.in + ((int64_t)min(n0 + q * 8 + g, A.N - 1) * A.in_stride + t * 8) * IN_BYTES;
 
     const uint32_t get = (uint32_t)__cvta_generic_to_shared(mine) + g * 128 + (g << 4) + t * 4;   // this lane's first word of the first slot
     int slot = 0;
@@ -250,8 +337,8 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_kernel(const Q4Args A)
     const unsigned short *e0, *e1;                         // the next stage's scales
     auto aim_scales = [&](int u) {
         const int r = u * ROWS + g;
-        e0 = A.scales + (size_t)min(r, V - 1) * n_groups;
-        e1 = A.scales + (size_t)min(r + 8, V - 1) * n_groups;
+        e0 = A.scales + (size_t)min(r, V - 1) * n_groups + first * (WIDE / GB);
+        e1 = A.scales + (size_t)min(r + 8, V - 1) * n_groups + first * (WIDE / GB);
     };
     auto load_scales = [&](int s) {
 #pragma unroll
@@ -264,16 +351,18 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_kernel(const Q4Args A)
         }
         e0 += WIDE / GB; e1 += WIDE / GB;
     };
-    int u = blockIdx.x + warp * gridDim.x;
-    if (u < units) { aim_scales(u); load_scales(0); }
-    if (XS) __syncthreads();
+    int u = begin;
+    if (u < units) { aim_scales(u); load_scales(first); }
+    float4 *const parts = (float4 *)(inputs + (XS ? H * 16 * NT * P : 0)) + lane;      // [warp][8 tokens][lane]
+    __syncthreads();
     for (; u < units; u += step) {
         float total[NT][4] = {};
-        uint32_t xs = (uint32_t)__cvta_generic_to_shared(inputs) + lane * 16;
-        for (int s = 0; s < stages; ++s) {
+        uint32_t xs = (uint32_t)__cvta_generic_to_shared(inputs) + lane * 16 + first * (WIDE * NT * P * 512);
+        const float2 *begin_at = (const float2 *)starts + first * (WIDE / GB) * NT * 4 + t;
+        for (int s = first; s < last; ++s) {
             const Scales<GB> s0[2] = {next0[0], next0[1]}, s1[2] = {next1[0], next1[1]};
-            if (s + 1 < stages) load_scales(s + 1);
-            else if (u + step < units) { aim_scales(u + step); load_scales(0); }
+            if (s + 1 < last) load_scales(s + 1);
+            else if (u + step < units) { aim_scales(u + step); load_scales(first); }
             cp_wait<WIDE_RING - 2>();
             __syncwarp();
             fetch();
@@ -289,15 +378,21 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_kernel(const Q4Args A)
                             b[q][p][0] = v.x; b[q][p][1] = v.y; b[q][p][2] = v.z; b[q][p][3] = v.w;
                         }
                     } else {
-                        load_inputs<P>(x[q] + (size_t)(s * WIDE + j) * 32 * IN_BYTES, has[q], b[q]);
+                        float x[8];
+                        load_columns<F32>(x_at[q] + (size_t)(s * WIDE + j) * 32 * IN_BYTES, n0 + q * 8 + g < A.N, x);
+                        cut_columns<P>(x, Token(largest(q * 8 + g)), b[q]);
+                    }
+                    if (j % GB == 0) {
+                        const float2 v = begin_at[(j / GB * NT + q) * 4];
+                        sum[q][0] = sum[q][2] = v.x; sum[q][1] = sum[q][3] = v.y;
                     }
                 }
                 const uint32_t w0 = lds32((get + slot) ^ (j << 4)), w1 = lds32(((get + slot) ^ (j << 4)) + 8 * 128);
-                const uint32_t a0[4] = {unpack<0>(w0, A.bf16_128), unpack<0>(w1, A.bf16_128), unpack<1>(w0, A.bf16_128), unpack<1>(w1, A.bf16_128)};
-                const uint32_t a1[4] = {unpack<2>(w0, A.bf16_128), unpack<2>(w1, A.bf16_128), unpack<3>(w0, A.bf16_128), unpack<3>(w1, A.bf16_128)};
+                const uint32_t v0 = w0 >> 8, v1 = w1 >> 8;
+                const uint32_t a0[4] = {w0 & CODE, w1 & CODE, w0 & CODE16, w1 & CODE16};
+                const uint32_t a1[4] = {v0 & CODE, v1 & CODE, v0 & CODE16, v1 & CODE16};
 #pragma unroll
                 for (int q = 0; q < NT; ++q) {
-                    if (j % GB == 0) sum[q][0] = sum[q][1] = sum[q][2] = sum[q][3] = 0.f;
 #pragma unroll
                     for (int p = 0; p < P; ++p) {
                         mma(sum[q], a0, b[q][p][0], b[q][p][1]);
@@ -319,14 +414,35 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_kernel(const Q4Args A)
                     if (s * WIDE + j < blocks) block(j);
             }
             xs += WIDE * NT * P * 512;
+            begin_at += WIDE / GB * NT * 4;
             slot = slot + WIDE_STAGE == WIDE_RING * WIDE_STAGE ? 0 : slot + WIDE_STAGE;
+        }
+        if (ks > 1) {
+            if (sub > 0) {
+#pragma unroll
+                for (int q = 0; q < NT; ++q)
+                    parts[(warp * NT + q) * 32] = make_float4(total[q][0], total[q][1], total[q][2], total[q][3]);
+            }
+            asm volatile("bar.sync %0, %1;" ::"r"(1 + warp / ks), "r"(32 * ks) : "memory");
+            if (sub == 0) {
+                for (int w = 1; w < ks; ++w)
+#pragma unroll
+                    for (int q = 0; q < NT; ++q) {
+                        const float4 v = parts[((warp + w) * NT + q) * 32];
+                        total[q][0] += v.x; total[q][1] += v.y; total[q][2] += v.z; total[q][3] += v.w;
+                    }
+            }
+            asm volatile("bar.sync %0, %1;" ::"r"(1 + warp / ks), "r"(32 * ks) : "memory");
+            if (sub > 0) continue;
         }
 #pragma unroll
         for (int q = 0; q < NT; ++q)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const int n = n0 + q * 8 + 2 * t + (k & 1), v = u * ROWS + g + (k >> 1) * 8;
-                if (n < A.N && v < V) store(A, n, v, total[q][k]);
+                const int m = q * 8 + 2 * t + (k & 1), n = n0 + m, v = u * ROWS + g + (k >> 1) * 8;
+                if (n >= A.N || v >= V) continue;
+                const uint32_t l = largest(m);
+                store(A, n, v, l < 0x7F800000u ? scaled_back(total[q][k], l) : one_logit<F32>(A, n, v, 32 * GB));
             }
     }
     cp_wait<0>();
@@ -494,30 +610,36 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
     if (split > 1) { od_cluster_arrive(); od_cluster_wait(); }
 }
 
-constexpr int ring_bytes = WARPS * RING * STAGE, wide_bytes = WARPS * WIDE_RING * WIDE_STAGE;
+constexpr int ring_bytes = WARPS * RING * STAGE, wide_bytes = F_WARPS * WIDE_RING * WIDE_STAGE;
+template <int NT> constexpr int part_bytes = F_WARPS * NT * 512;
 template <int NT> constexpr int grad_bytes = WARPS * 8 * NT * COLS * 4 > ring_bytes ? WARPS * 8 * NT * COLS * 4 : ring_bytes;
 
 typedef void (*Kernel)(Q4Args);
-struct Variant { Kernel kernel; int smem, tokens; };
+struct Variant { Kernel kernel; int smem, tokens, threads = F_THREADS; };
 
 // Forward: 8, 16 or 32 tokens to a block, the most (and no more than there are) whose inputs fit into shared memory
 // beside the rings; where those of 8 do not, they stay in global memory. Backward: 8 or 16.
-constexpr int IN_SMEM = 227 * 1024 - wide_bytes;
-template <int P, int NT, int GB>
-Variant in_smem(int32_t H) { return {od_q4_kernel<P, NT, GB, true>, wide_bytes + H * 16 * NT * P, 8 * NT}; }
+template <int P, int NT, int GB, bool XS>
+Variant forward_kernel(int32_t H)
+{
+    return {od_q4_kernel<P, NT, GB, XS>, wide_bytes + part_bytes<NT> + H / GB * NT + (XS ? H * 16 * NT * P : 0), 8 * NT};
+}
+constexpr int SMEM_MOST = 226 * 1024;                      // (and a little of fixed size)
 template <int GB>
 Variant forward_of(bool f32, int N, int32_t H)
 {
-    if (f32) return H <= IN_SMEM / 48 ? in_smem<3, 1, GB>(H) : Variant{od_q4_kernel<3, 1, GB, false>, wide_bytes, 8};
-    if (N > 16 && H <= IN_SMEM / 64) return in_smem<1, 4, GB>(H);
-    if (N > 8 && H <= IN_SMEM / 32) return in_smem<1, 2, GB>(H);
-    return H <= IN_SMEM / 16 ? in_smem<1, 1, GB>(H) : Variant{od_q4_kernel<1, 1, GB, false>, wide_bytes, 8};
+    Variant v = f32 ? forward_kernel<3, 1, GB, true>(H) : N > 16 ? forward_kernel<1, 4, GB, true>(H)
+              : N > 8 ? forward_kernel<1, 2, GB, true>(H) : forward_kernel<1, 1, GB, true>(H);
+    if (v.smem > SMEM_MOST && !f32 && N > 16) v = forward_kernel<1, 2, GB, true>(H);
+    if (v.smem > SMEM_MOST && !f32) v = forward_kernel<1, 1, GB, true>(H);
+    if (v.smem <= SMEM_MOST) return v;
+    return f32 ? forward_kernel<3, 1, GB, false>(H) : forward_kernel<1, 1, GB, false>(H);
 }
 template <int GB>
 Variant backward_of(bool f32, int N)
 {
-    if (f32) return N <= 8 ? Variant{od_q4_grad_kernel<3, 1, GB>, grad_bytes<1>, 8} : Variant{od_q4_grad_kernel<3, 2, GB>, grad_bytes<2>, 16};
-    return N <= 8 ? Variant{od_q4_grad_kernel<2, 1, GB>, grad_bytes<1>, 8} : Variant{od_q4_grad_kernel<2, 2, GB>, grad_bytes<2>, 16};
+    if (f32) return N <= 8 ? Variant{od_q4_grad_kernel<3, 1, GB>, grad_bytes<1>, 8, THREADS} : Variant{od_q4_grad_kernel<3, 2, GB>, grad_bytes<2>, 16, THREADS};
+    return N <= 8 ? Variant{od_q4_grad_kernel<2, 1, GB>, grad_bytes<1>, 8, THREADS} : Variant{od_q4_grad_kernel<2, 2, GB>, grad_bytes<2>, 16, THREADS};
 }
 Variant variant(bool backward, int32_t G, bool f32, int N, int32_t H)
 {
@@ -528,7 +650,7 @@ Variant variant(bool backward, int32_t G, bool f32, int N, int32_t H)
 void configure(cudaLaunchConfig_t &cfg, cudaLaunchAttribute (&attr)[2], const Variant &v, unsigned blocks, unsigned tiles, unsigned cluster)
 {
     cfg = {};
-    cfg.gridDim = dim3(blocks, tiles); cfg.blockDim = dim3(THREADS);
+    cfg.gridDim = dim3(blocks, tiles); cfg.blockDim = dim3(v.threads);
     cfg.dynamicSmemBytes = v.smem;
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
@@ -547,7 +669,7 @@ cudaError_t od_q4_prepare_device(int32_t (*clusters)[OD_Q4_MAX_SPLIT + 1])
             for (int f32 = 0; f32 < 2; ++f32)
                 for (int N = 8; N <= 64; N *= 2) {         // (64: none in shared memory)
                     const Variant v = variant(backward, G, f32, N, N == 64 ? 65536 : 128);
-                    cudaError_t e = cudaFuncSetAttribute((const void *)v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+                    cudaError_t e = cudaFuncSetAttribute((const void *)v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST);
                     if (e == cudaSuccess && backward) e = cudaFuncSetAttribute((const void *)v.kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
                     if (e != cudaSuccess) return e;
                 }
@@ -572,11 +694,18 @@ cudaError_t od_launch_q4(const od_ctx *c, bool backward, int32_t N, int32_t V, i
 {
     const Variant v = variant(backward, G, a_dtype == OD_F32, N, H);
     Q4Args args = {a, as, (const uint8_t *)codes, (const unsigned short *)scales, b, bs, N, V, H, a_dtype == OD_F32, b_dtype == OD_F32,
-                   H % COLS == 0 && ((uintptr_t)scales & 7u) == 0, 0x43004300u, 1, 1};
+                   H % COLS == 0 && ((uintptr_t)scales & 7u) == 0, 0x43004300u, 1, 1, 1};
     unsigned blocks;
     if (!backward) {
         const int64_t units = ((int64_t)V + ROWS - 1) / ROWS;
         blocks = (unsigned)(units < c->sm_count ? units : c->sm_count);
+        // Warps to the same 16 rows (1, 2, 4): the fewest stages in a row of one warp, of equal ones the fewest warps
+        const int64_t each = (units + blocks - 1) / blocks, stages = (H + 32 * WIDE - 1) / (32 * WIDE);
+        int64_t best = INT64_MAX;
+        for (int32_t ks = 1; ks <= 4 && ks <= stages; ks *= 2) {
+            const int64_t cost = (each * ks + F_WARPS - 1) / F_WARPS * ((stages + ks - 1) / ks);
+            if (cost < best) { best = cost; args.k_split = ks; }
+        }
     } else {
         // How many warps side by side (4, 2, 1) and blocks to a cluster (any number that the device holds): the fewest
         // rounds of clusters times rows of a warp; of equal ones the widest rows.

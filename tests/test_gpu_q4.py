@@ -2,10 +2,11 @@
 
 Tolerances. A product of an input and a code is exact (an fp32 input is taken in three bf16 pieces, a scaled bf16 one in
 two), so the errors are those of fp32 sums: a matrix instruction adds sixteen products to its accumulator with an
-error of at most 2^-22 of the largest sum of magnitudes it meets, an fp32 step 2^-24. With S = sum |x w| a logit
-goes through group / 16 * 3 instructions per group and one step per group; a gradient through at most
-vocab / 16 * 3 instructions, one rounding of each scaled input, and the steps that join the parts (below 64).
-The result is rounded once to its type.
+error of at most 2^-22 of the largest sum of magnitudes it meets, an fp32 step 2^-24. The instructions add x u, the 8 that is
+to be taken off a code is in what a group's sum begins at: the magnitudes are those of x u s and 8 x s, S = sum |x s| (u + 8).
+A logit goes through group / 16 * 3 instructions per group and one step per group, its group's beginning through
+group / 8 + 2 fp32 steps; a gradient through at most vocab / 16 * 3 instructions, one rounding of each scaled input, and the
+steps that join the parts (below 64). The result is rounded once to its type.
 """
 import math
 
@@ -57,14 +58,19 @@ def same(got, want, tol):
     assert not bad.any(), f"{int(bad.sum())} of {bad.numel()}: {got[bad][:4].tolist()} for {want[bad][:4].tolist()}, tolerance {tol[bad][:4].tolist()}"
 
 
-def check_logits(got, x, w, G):
-    want, size = x.double() @ w.T, x.double().abs() @ w.abs().T
-    tol = size * (G / 16 * 3 * 2.0 ** -22 + (w.shape[1] / G + 4) * 2.0 ** -24)
+def magnitudes(codes, scales):
+    """(u + 8) |s| of every weight."""
+    return weights(codes, torch.ones_like(scales)).add_(16) * scales.double().abs().repeat_interleave(2 * codes.shape[1] // scales.shape[1], 1)
+
+
+def check_logits(got, x, w, G, size_of):
+    want, size = x.double() @ w.T, x.double().abs() @ size_of.T
+    tol = size * (G / 16 * 3 * 2.0 ** -22 + (G / 8 + 2 + w.shape[1] / G + 4) * 2.0 ** -24)
     same(got, want, tol + HALF[got.dtype] * (want.abs() + tol))
 
 
-def check_grad(got, dy, w):
-    want, size = dy.double() @ w, dy.double().abs() @ w.abs()
+def check_grad(got, dy, w, size_of):
+    want, size = dy.double() @ w, dy.double().abs() @ size_of
     tol = size * (math.ceil(w.shape[0] / 16) * 3 * 2.0 ** -22 + 64 * 2.0 ** -24)
     same(got, want, tol + HALF[got.dtype] * (want.abs() + tol))
 
@@ -85,7 +91,7 @@ def test_logits(ctx, N, V, H, G, given, made):
     per = 16 // torch.empty(0, dtype=made).element_size()
     store = torch.full((N + 1, (V // per + 2) * per), 55.0, dtype=made, device="cuda")
     out = od.od_q4_logits(ctx, x, codes, scales, out=store[:N, :V])
-    check_logits(out, x, weights(codes, scales), G)
+    check_logits(out, x, weights(codes, scales), G, magnitudes(codes, scales))
     assert (store[N] == 55).all() and (store[:, V:] == 55).all()
     assert torch.equal(out, od.od_q4_logits(ctx, x, codes, scales, dtype=made))      # the same in every run
 
@@ -98,7 +104,7 @@ def test_gradient(ctx, N, V, H, G, given, made):
     dy = padded(torch.randn(N, V, generator=g, device="cuda").to(given))
     store = torch.full((N + 1, H + 32), 55.0, dtype=made, device="cuda")
     out = od.od_q4_logits_grad(ctx, dy, codes, scales, out=store[:N, :H])
-    check_grad(out, dy, weights(codes, scales))
+    check_grad(out, dy, weights(codes, scales), magnitudes(codes, scales))
     assert (store[N] == 55).all() and (store[:, H:] == 55).all()
     assert torch.equal(out, od.od_q4_logits_grad(ctx, dy, codes, scales, dtype=made))
 
@@ -143,7 +149,7 @@ def test_inputs_at_the_limits(ctx, dtype):
     sign = torch.sign(w[:, 6])
     assert torch.equal(y[1], (sign * math.inf).float()) and torch.equal(y[2], (-sign * math.inf).float()) and torch.isnan(y[3]).all()
     keep = [0, 4, 5, 6, 7, 8]
-    check_logits(y[keep], x[keep], w, G)
+    check_logits(y[keep], x[keep], w, G, magnitudes(codes, scales))
     dy = padded(torch.randn(N, V, device="cuda").to(dtype))
     codes[4] = 0x99
     w = weights(codes, scales)
@@ -151,15 +157,16 @@ def test_inputs_at_the_limits(ctx, dtype):
     dx = od.od_q4_logits_grad(ctx, dy, codes, scales)
     assert torch.equal(dx[1], (torch.sign(w[4]) * math.inf).float()) and torch.isnan(dx[2]).all()
     keep = [0] + list(range(3, N))
-    check_grad(dx[keep], dy[keep], w)
+    check_grad(dx[keep], dy[keep], w, magnitudes(codes, scales))
     # the type's largest value, and tiny ones, through weights of a half
     codes.fill_(0x88); codes[:, 0] = 0x89; scales.fill_(0.5)
     x = torch.zeros(2, H, device="cuda", dtype=dtype)
     x[0, 0], x[1, 0] = torch.finfo(dtype).max, 2.0 ** -126
-    assert torch.equal(od.od_q4_logits(ctx, x, codes, scales), (x[:, :1].double() / 2).float().expand(2, V))
+    # (a product x u with u = 9, a beginning of -8 x: the six instructions of its group in fp32 meet 17 x at most)
+    check_logits(od.od_q4_logits(ctx, x, codes, scales), x, weights(codes, scales), G, magnitudes(codes, scales))
     dy = padded(torch.zeros(2, V, device="cuda", dtype=dtype))
     dy[0, 3], dy[1, 3] = torch.finfo(dtype).max, 2.0 ** -110
-    assert torch.equal(od.od_q4_logits_grad(ctx, dy, codes, scales)[:, 0], (dy[:, 3].double() / 2).float())
+    check_grad(od.od_q4_logits_grad(ctx, dy, codes, scales), dy, weights(codes, scales), magnitudes(codes, scales))
 
 
 def test_the_gradient_is_the_transpose(ctx):
@@ -170,7 +177,7 @@ def test_the_gradient_is_the_transpose(ctx):
     a = (od.od_q4_logits(ctx, x, codes, scales).double() * dy.double()).sum()
     b = (od.od_q4_logits_grad(ctx, dy, codes, scales).double() * x.double()).sum()
     w = weights(codes, scales)
-    size = float((x.double().abs() @ w.abs().T * dy.double().abs()).sum())
+    size = float((x.double().abs() @ magnitudes(codes, scales).T * dy.double().abs()).sum())
     assert abs(float(a - b)) <= size * (2.0 ** -17 + math.ceil(V / 16) * 3 * 2.0 ** -22)
 
 
@@ -182,10 +189,10 @@ def test_codes_past_32_bits(ctx):
     x = torch.randn(1, H, device="cuda").to(BF16)
     y = od.od_q4_logits(ctx, x, codes, scales)
     rows = torch.tensor([0, 1, 32767, 32768, 65535, 65536, 69998, V - 1], device="cuda")
-    check_logits(y[:, rows], x, weights(codes[rows], scales[rows]), G)
+    check_logits(y[:, rows], x, weights(codes[rows], scales[rows]), G, magnitudes(codes[rows], scales[rows]))
     dy = padded(torch.zeros(1, V, device="cuda"))
     dy[0, rows] = torch.randn(len(rows), device="cuda")
-    check_grad(od.od_q4_logits_grad(ctx, dy, codes, scales), dy[:, rows], weights(codes[rows], scales[rows]))
+    check_grad(od.od_q4_logits_grad(ctx, dy, codes, scales), dy[:, rows], weights(codes[rows], scales[rows]), magnitudes(codes[rows], scales[rows]))
 
 
 def test_batches_of_rows_captured_and_replayed_on_another_stream(ctx):
@@ -206,8 +213,8 @@ def test_batches_of_rows_captured_and_replayed_on_another_stream(ctx):
         x.copy_(torch.randn(B, K, H, device="cuda"))
         graph.replay()
     torch.cuda.synchronize()
-    check_logits(logits.reshape(-1, V), x.view(-1, H), w, G)
-    check_grad(back.view(-1, H), logits.reshape(-1, V), w)
+    check_logits(logits.reshape(-1, V), x.view(-1, H), w, G, magnitudes(codes, scales))
+    check_grad(back.view(-1, H), logits.reshape(-1, V), w, magnitudes(codes, scales))
 
 
 def test_a_training_step_of_the_drafter(ctx):
@@ -234,7 +241,7 @@ def test_a_training_step_of_the_drafter(ctx):
     loss = (a * torch.gather(ref, 2, ids.long()[:, :, None]).squeeze(2) - b * (ref.exp() * ref).sum(2) + (c * top).sum(2))[live].sum()
     loss.backward()
     # the logits' errors (group sums of |x w|) through a softmax, then the tolerances of the two gradients
-    size = float((hidden.double().abs() @ w.abs().T).max())
+    size = float((hidden.double().abs() @ magnitudes(codes, scales).T).max())
     spread = (a.abs() + 16 * b.abs() + c.abs().sum(2)).double()[:, :, None] * w.abs().max() * 2 / T.double()[:, None, None]
     tol = spread * (size * 2.0 ** -18 * 4 + 2.0 ** -14)
     assert ((got.double() - h.grad).abs() <= tol)[live].all()
