@@ -451,6 +451,12 @@ def _shaped(t: Optional[torch.Tensor], shape, what: str):
 def od_token_logprobs(ctx: Context, logits, ids=None, temperature=None, n_rows=None, n_top: int = 0,
                       out: Optional[LogprobOut] = None) -> LogprobOut:
     """Log probability of ids [B, R] (-1 = none), entropy and the n_top likeliest tokens of logit rows [B, R, V]."""
+    if out is not None:
+        status = _native.token_logprobs(ctx.address, ctx.index, n_top, logits, ids, temperature, n_rows, out.logprob, out.entropy,
+                                        out.row_max, out.row_sum, out.top_ids, out.top_logprobs, out.flags)
+        if status is not None:
+            _check(status, "od_token_logprobs")
+            return out
     d, i32, f32 = ctx.device, torch.int32, torch.float32
     B, R, V, rs, ss = _row_strides(logits, d, "logits")
     out = out or alloc_logprob_out(ctx, B, R, n_top)
@@ -469,6 +475,12 @@ def od_token_logprobs_grad(ctx: Context, logits, ids, lp: LogprobOut, g_logprob=
                            temperature=None, n_rows=None, grad=None):
     """The gradient with respect to the logits from those of the log probabilities [B, R], the entropies [B, R]
     and the alternatives' log probabilities [B, R, n]; grad may be the logits themselves."""
+    if grad is not None:
+        status = _native.token_logprobs_grad(ctx.address, ctx.index, logits, ids, temperature, n_rows, lp.row_max, lp.row_sum,
+                                             lp.entropy, lp.top_ids, g_logprob, g_entropy, g_top, grad)
+        if status is not None:
+            _check(status, "od_token_logprobs_grad")
+            return grad
     d, i32, f32 = ctx.device, torch.int32, torch.float32
     B, R, V, rs, ss = _row_strides(logits, d, "logits")
     if grad is None:
@@ -510,6 +522,13 @@ def _flat_rows(t: torch.Tensor, width: int, device, what: str):
 
 
 def _q4(ctx: Context, x, codes, scales, out, dtype, backward: bool):
+    name = "od_q4_logits_grad" if backward else "od_q4_logits"
+    if out is not None:
+        native = _native.q4_logits_grad if backward else _native.q4_logits
+        status = native(ctx.address, ctx.index, x, codes, scales, out)
+        if status is not None:
+            _check(status, name)
+            return out
     d = ctx.device
     V, H = int(codes.shape[0]), int(codes.shape[1]) * 2
     if codes.dim() != 2 or scales.dim() != 2 or scales.shape[0] != V or scales.shape[1] < 1 or H % scales.shape[1]:
@@ -522,7 +541,6 @@ def _q4(ctx: Context, x, codes, scales, out, dtype, backward: bool):
         raise ValueError("the rows of out must be those of the input")
     n, xs = _flat_rows(x, wide, d, "g_logits" if backward else "hidden")
     _, ys = _flat_rows(out, wide_out, d, "out")
-    name = "od_q4_logits_grad" if backward else "od_q4_logits"
     _check(getattr(lib(), name)(
         ctx.handle, n, V, H, H // int(scales.shape[1]), C.c_void_p(x.data_ptr()), logit_dtype_code(x), xs,
         _dp(codes, torch.uint8, d), _dp(scales, torch.bfloat16, d), C.c_void_p(out.data_ptr()), logit_dtype_code(out),

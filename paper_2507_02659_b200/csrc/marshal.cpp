@@ -207,6 +207,117 @@ PyObject *distill_loss(PyObject *, PyObject *const *a, Py_ssize_t n)
     return call(x, od_distill_loss, args);
 }
 
+// rows [B, R, V] (or [N, V] as one sequence) with dense rows of whole 16-byte strides, in their order
+struct Rows {
+    void *p = nullptr;
+    int32_t dtype = 0;
+    int64_t B = 0, R = 0, V = 0, row_stride = 0, seq_stride = 0;
+    Rows(Args &x, const at::Tensor *t)
+    {
+        const int64_t d = t ? t->dim() : 0;
+        if ((d != 2 && d != 3) || t->numel() == 0 || (t->size(d - 1) > 1 && t->stride(d - 1) != 1) ||
+            (t->scalar_type() != c10::kFloat && t->scalar_type() != c10::kBFloat16)) {
+            x.ok = false;
+            return;
+        }
+        p = t->data_ptr();
+        dtype = t->scalar_type() == c10::kFloat ? OD_F32 : OD_BF16;
+        B = d == 3 ? t->size(0) : 1; R = t->size(d - 2); V = t->size(d - 1);
+        // (torch gives a dimension of one entry any stride)
+        const int64_t esz = dtype == OD_F32 ? 4 : 2;
+        row_stride = R > 1 ? t->stride(d - 2) : B > 1 ? t->stride(0) : (V * esz + 15) / 16 * 16 / esz;
+        seq_stride = B > 1 ? t->stride(0) : row_stride * R;
+        if (B > INT32_MAX || R > INT32_MAX || V > INT32_MAX) x.ok = false;
+    }
+    // a call that knows rows only: all of them equally far apart
+    int32_t count(Args &x) const
+    {
+        if (seq_stride != row_stride * R || B * R > INT32_MAX) x.ok = false;
+        return (int32_t)(B * R);
+    }
+};
+template <typename T>
+T *shaped(Args &x, c10::ScalarType type, c10::IntArrayRef shape, bool may_be_none = false)
+{
+    const at::Tensor *t = x.tensor(may_be_none);
+    if (!t) return nullptr;
+    if (t->scalar_type() != type || t->sizes() != shape || !t->is_contiguous()) { x.ok = false; return nullptr; }
+    return (T *)t->data_ptr();
+}
+
+PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Args x(a, n, 14);
+    od_ctx *c = x.ctx();
+    const int32_t n_top = x.i32();
+    const Rows l(x, x.tensor());
+    const int64_t br[] = {l.B, l.R}, top[] = {l.B, l.R, n_top}, b[] = {l.B};
+    const int32_t *ids = shaped<int32_t>(x, c10::kInt, br, true);
+    const float *T = shaped<float>(x, c10::kFloat, b, true);
+    const int32_t *n_rows = shaped<int32_t>(x, c10::kInt, b, true);
+    float *f[4];
+    for (float *&p : f) p = shaped<float>(x, c10::kFloat, br);
+    int32_t *top_ids = shaped<int32_t>(x, c10::kInt, top);
+    float *top_lp = shaped<float>(x, c10::kFloat, top);
+    uint32_t *flags = shaped<uint32_t>(x, c10::kInt, br);
+    std::tuple args{c, (int32_t)l.B, (int32_t)l.R, (int32_t)l.V, (const void *)l.p, l.dtype, l.row_stride, l.seq_stride, ids, n_rows, T,
+                    n_top, f[0], f[1], f[2], f[3], top_ids, top_lp, flags};
+    return call(x, od_token_logprobs, args);
+}
+
+PyObject *token_logprobs_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Args x(a, n, 14);
+    od_ctx *c = x.ctx();
+    const Rows l(x, x.tensor());
+    const int64_t br[] = {l.B, l.R}, b[] = {l.B};
+    const int32_t *ids = shaped<int32_t>(x, c10::kInt, br, true);
+    const float *T = shaped<float>(x, c10::kFloat, b, true);
+    const int32_t *n_rows = shaped<int32_t>(x, c10::kInt, b, true);
+    const float *mx = shaped<float>(x, c10::kFloat, br), *sum = shaped<float>(x, c10::kFloat, br), *H = shaped<float>(x, c10::kFloat, br);
+    const at::Tensor *top_ids = x.tensor();
+    const float *g_lp = shaped<float>(x, c10::kFloat, br, true), *g_h = shaped<float>(x, c10::kFloat, br, true);
+    const at::Tensor *g_top = x.tensor(true);
+    const Rows g(x, x.tensor());
+    if (g.B != l.B || g.R != l.R || g.V != l.V || g.dtype != l.dtype) x.ok = false;
+    int32_t n_top = 0;
+    if (x.ok && g_top) {
+        if (!top_ids || g_top->dim() != 3 || g_top->size(0) != l.B || g_top->size(1) != l.R || top_ids->sizes() != g_top->sizes() ||
+            g_top->scalar_type() != c10::kFloat || top_ids->scalar_type() != c10::kInt || !g_top->is_contiguous() ||
+            !top_ids->is_contiguous() || g_top->size(2) > INT32_MAX)
+            x.ok = false;
+        else
+            n_top = (int32_t)g_top->size(2);
+    }
+    if (!x.ok) Py_RETURN_NONE;
+    std::tuple args{c, (int32_t)l.B, (int32_t)l.R, (int32_t)l.V, (const void *)l.p, l.dtype, l.row_stride, l.seq_stride, ids, n_rows, T,
+                    mx, sum, H, n_top, n_top ? (const int32_t *)top_ids->data_ptr() : nullptr, g_lp, g_h,
+                    n_top ? (const float *)g_top->data_ptr() : nullptr, g.p, g.row_stride, g.seq_stride};
+    return call(x, od_token_logprobs_grad, args);
+}
+
+template <bool BACKWARD>
+PyObject *q4(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    Args x(a, n, 6);
+    od_ctx *c = x.ctx();
+    const at::Tensor *in_t = x.tensor();
+    const Rows in(x, in_t);
+    const at::Tensor *codes = x.tensor(), *scales = x.tensor(), *out_t = x.tensor();
+    const Rows out(x, out_t);
+    if (!x.ok || codes->dim() != 2 || scales->dim() != 2 || codes->scalar_type() != c10::kByte || scales->scalar_type() != c10::kBFloat16 ||
+        !codes->is_contiguous() || !scales->is_contiguous())
+        Py_RETURN_NONE;
+    const int64_t V = codes->size(0), H = codes->size(1) * 2, groups = scales->size(1);
+    if (scales->size(0) != V || groups < 1 || H % groups != 0 || V > INT32_MAX || H > INT32_MAX || in.V != (BACKWARD ? V : H) ||
+        out.V != (BACKWARD ? H : V) || in_t->dim() != out_t->dim() || in.B != out.B || in.R != out.R)
+        Py_RETURN_NONE;
+    out.count(x);
+    std::tuple args{c, in.count(x), (int32_t)V, (int32_t)H, (int32_t)(H / groups), (const void *)in.p, in.dtype, in.row_stride,
+                    (const void *)codes->data_ptr(), (const void *)scales->data_ptr(), out.p, out.dtype, out.row_stride};
+    return call(x, BACKWARD ? od_q4_logits_grad : od_q4_logits, args);
+}
+
 PyObject *verify_shard_stats(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     Args x(a, n, 11);
@@ -284,6 +395,9 @@ PyObject *guarded(PyObject *self, PyObject *const *a, Py_ssize_t n)
 PyMethodDef methods[] = {METHOD(map_proposals), METHOD(verify), METHOD(sample_residual), METHOD(step), METHOD(exit_rule),
                          METHOD(distill_loss), METHOD(verify_shard_stats), METHOD(verify_shard_finish),
                          METHOD(sample_shard_mass), METHOD(sample_shard_pick), METHOD(cache_insert), METHOD(cache_trim),
+                         METHOD(token_logprobs), METHOD(token_logprobs_grad),
+                         {"q4_logits", (PyCFunction)(void (*)(void))guarded<q4<false>>, METH_FASTCALL, nullptr},
+                         {"q4_logits_grad", (PyCFunction)(void (*)(void))guarded<q4<true>>, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
