@@ -46,7 +46,7 @@ int32_t dev_alloc(T **p, size_t n)
 void free_all(od_ctx *c)
 {
     od_cache_free_dynamic(c);
-    void *ptrs[] = {c->d_vocab_map, c->d_inv_map, c->d_map_serial, c->d_distill_lists, c->d_sample_lists, c->d_keys, c->d_vals, c->d_partials,
+    void *ptrs[] = {c->d_vocab_map, c->d_inv_map, c->d_map_serial, c->d_distill_lists, c->d_sample_lists, c->d_keys, c->d_vals, c->d_partials, c->d_q4_parts,
                     c->d_tile_sums, c->s_logits, c->s_q_rows, c->s_q_sel, c->s_temperature,
                     c->s_draft_ids, c->s_draft_len, c->s_seed, c->s_tgt_ids, c->s_span_start,
                     c->s_span_len, c->s_m, c->s_n_acc, c->s_n_draft, c->s_token, c->s_q_prime,
@@ -141,7 +141,6 @@ bool prepare_kernels(od_ctx *c)
     struct Resident {
         unsigned long long context;
         int32_t sample[OD_SAMPLE_LEVELS], step[OD_SAMPLE_LEVELS], shard[OD_SHARD_SIZES][OD_SAMPLE_MAX_PARTS + 1], distill[OD_DISTILL_LEVELS];
-        int32_t q4[2][OD_Q4_MAX_SPLIT + 1];
     };
     constexpr int DEVICES = 64;
     static std::mutex mutex;
@@ -153,14 +152,13 @@ bool prepare_kernels(od_ctx *c)
     if (id == 0 || r.context != id) {
         r.context = 0;
         if (od_sample_prepare_device(r.sample, r.shard) != cudaSuccess || od_step_prepare_device(r.step) != cudaSuccess ||
-            od_q4_prepare_device(r.q4) != cudaSuccess) return false;
+            od_q4_prepare_device() != cudaSuccess) return false;
         od_distill_resident(r.distill);
         r.context = id;
     }
     memcpy(c->sample_clusters, r.sample, sizeof(r.sample));
     memcpy(c->step_clusters, r.step, sizeof(r.step));
     memcpy(c->shard_clusters, r.shard, sizeof(r.shard));
-    memcpy(c->q4_clusters, r.q4, sizeof(r.q4));
     memcpy(c->distill_few_clusters, r.distill, sizeof(r.distill));
     return true;
 }
@@ -233,6 +231,7 @@ int32_t od_create(od_ctx **ctx, int32_t device, int32_t draft_vocab, int32_t tar
     if (st == OD_OK) st = dev_alloc(&lists, od_sample_lists_bytes(draft_vocab, target_vocab));
     c->d_sample_lists = lists;
     if (st == OD_OK) st = dev_alloc(&c->d_partials, rows * OD_VERIFY_SEG_MAX);
+    if (st == OD_OK) st = dev_alloc(&c->d_q4_parts, (size_t)c->sm_count * (OD_Q4_PART_BYTES / 4));
     if (st == OD_OK) st = dev_alloc(&c->d_tile_sums, (size_t)max_batch * c->tiles_per_row);
     if (st != OD_OK) {
         free_all(c);

@@ -23,14 +23,12 @@ namespace {
 
 constexpr int WARPS = 16, THREADS = 32 * WARPS;
 constexpr int F_WARPS = 16, F_THREADS = 32 * F_WARPS;
-constexpr int ROWS = 16;                                   // of a stage, and of a matrix instruction
-constexpr int COLS = 128;                                  // of a stage: four blocks of 32
-constexpr int STAGE = ROWS * COLS / 2;                     // bytes
-constexpr int RING = 6;                                    // stages of a warp
+constexpr int ROWS = 16;                                   // of a matrix instruction
+constexpr int COLS = 128;                                  // backward: of a warp, four blocks of 32
+constexpr int G_RING = 3;                                  // backward: stages of a warp
 constexpr int WIDE = 8;                                    // forward: blocks of 32 columns to a stage
 constexpr int WIDE_STAGE = ROWS * WIDE * 16;
 constexpr int WIDE_RING = 3;
-constexpr int MAX_SPLIT = OD_Q4_MAX_SPLIT;                 // blocks that share the rows of a gradient (a cluster)
 
 struct Q4Args {
     const void *in;                                        // x or dy
@@ -41,9 +39,10 @@ struct Q4Args {
     int64_t out_stride;
     int32_t N, V, H, in_f32, out_f32;
     int32_t wide_scales;                                   // the scales of a stage's row are one aligned word
-    uint32_t bf16_128;                                     // see unpack
     int32_t k_split;                                       // forward: warps to the same rows
-    int32_t split, col_warps;                              // backward: blocks of a cluster, warps side by side
+    int32_t split, col_warps;                              // backward: blocks on the same columns, warps side by side
+    int32_t first_token;
+    float *parts;                                          // the context's scratch
 };
 
 __device__ __forceinline__ void cp16(uint32_t to, const void *from)
@@ -64,28 +63,11 @@ __device__ __forceinline__ uint4 lds128(uint32_t at)
     asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
     return v;
 }
-__device__ __forceinline__ float lds_cluster(uint32_t at)
-{
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
-    return v;
-}
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// codes i and i + 4 of a word, less 8, as a pair of bf16: 128 + u has u in its last bits. (bf16_128, a pair of 128, is an
-// argument of the kernel: a mask and an or with two constants that the compiler knows are two instructions, and with one
-// in a register they are one.)
-template <int I>
-__device__ __forceinline__ uint32_t unpack(uint32_t w, uint32_t bf16_128)
-{
-    uint32_t m, d;
-    asm("lop3.b32 %0, %1, 0x000F000F, %2, 0xEA;" : "=r"(m) : "r"(w >> 4 * I), "r"(bf16_128));
-    asm("sub.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(m), "r"(0x43084308u));
-    return d;
 }
 __device__ __forceinline__ uint32_t halves(uint32_t a, uint32_t b, uint32_t pick)
 {
@@ -94,21 +76,15 @@ __device__ __forceinline__ uint32_t halves(uint32_t a, uint32_t b, uint32_t pick
 constexpr uint32_t CODE = 0x000F000Fu, CODE16 = 0x00F000F0u;
 constexpr uint32_t LOW = 0x5410, HIGH = 0x7632;            // both low halves, both high halves
 
-// x = hi + mid + lo by cutting its bits; of an infinity everything is in hi
-__device__ __forceinline__ void cut(float x, bool guard, float &rest)
-{
-    rest = x - __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
-    if (guard && fabsf(x) == INFINITY) rest = 0.f;
-}
-// P pieces of a pair as bf16 pairs
+// P pieces of a pair as bf16 pairs: the leading 8 bits of what is left, which are cut off it
 template <int P>
-__device__ __forceinline__ void pieces(float a, float b, bool guard, uint32_t (&out)[P])
+__device__ __forceinline__ void pieces(float a, float b, uint32_t (&out)[P])
 {
     out[0] = halves(__float_as_uint(a), __float_as_uint(b), HIGH);
 #pragma unroll
     for (int p = 1; p < P; ++p) {
-        cut(a, guard, a);
-        cut(b, guard, b);
+        a -= __uint_as_float(__float_as_uint(a) & 0xFFFF0000u);
+        b -= __uint_as_float(__float_as_uint(b) & 0xFFFF0000u);
         out[p] = halves(__float_as_uint(a), __float_as_uint(b), HIGH);
     }
 }
@@ -155,9 +131,6 @@ struct Scales {
         for (auto &x : w) x = 0;
     }
 };
-
-template <int P>
-__device__ __forceinline__ void pieces(float a, float b, uint32_t (&out)[P]) { pieces<P>(a, b, false, out); }
 
 // ---- forward: 16 rows of the weights to a warp, all columns -------------------------------------
 //
@@ -448,171 +421,238 @@ __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
     cp_wait<0>();
 }
 
-// ---- backward: 128 columns to a warp, every so many-th 16 rows ----------------------------------
+// ---- backward: 128 columns to a warp, every so many-th 32 rows ----------------------------------
 //
 // Rows are summed over: two of them are the pair of an operand, four columns in a row are a half word, so a block of 32
 // columns is the sixteen rows of two fragments. A lane reads the word that its half is in of four rows. The tokens' side is
-// made anew for each group: gradient times scale, in pieces. Warps side by side share rows (a block reads up to 256
-// bytes in a row); those on the same columns, and the blocks of a cluster, are summed at the end in a fixed order.
+// made anew for each group: gradient times scale, in pieces. It is scaled by 2^110 for what the codes are as bf16 numbers;
+// what is too large for that (and infinities and NaN) is added to the sums on its own. The 8 of a code is taken off at the
+// end: sums of gradient times scale, of which a lane has those of its rows.
+// Warps side by side share rows (a block reads up to 256 bytes in a row). Those on the same columns are summed at the end,
+// and the blocks on the same columns by a second kernel, from the context's scratch: both in a fixed order. (In
+// clusters the blocks do not fill the device: 96 of 148 multiprocessors for 16 tiles of columns.)
+constexpr float UP = 0x1p110f, BACK = 0x1p23f;             // 2^110 2^-133 2^23 = 1
+constexpr int G_ROWS = 32;                                 // of a stage
+constexpr int G_CODES = G_ROWS * COLS / 2;                 // bytes
+
+__device__ __forceinline__ void cp16_part(uint32_t to, const void *from, int bytes)    // the rest is zeros
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+
+template <int P, int NT> constexpr int g_stage = G_CODES + 8 * NT * G_ROWS * (P == 3 ? 4 : 2);
+template <int P, int NT, int GB> constexpr int g_warp = G_RING * g_stage<P, NT> + 2 * G_ROWS * (4 / GB) * 4;
+
 template <int P, int NT, int GB>
 __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
 {
     extern __shared__ __align__(128) unsigned char smem[];
+    constexpr bool F32 = P == 3;
+    constexpr int ESZ = F32 ? 4 : 2, GROUPS = 4 / GB, PIECES = G_ROWS * ESZ / 16, STAGE = g_stage<P, NT>;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x >> 5, 0);
     const int H = A.H, V = A.V, cw = A.col_warps, split = A.split;
     const int rank = blockIdx.x % split, tile = blockIdx.x / split;
     const int col = (tile * cw + warp % cw) * COLS, here = max(0, min(4, (H - col) / 32)), n_groups = H / (32 * GB);
     const int slabs = split * (WARPS / cw), slab = rank * (WARPS / cw) + warp / cw;
-    const int steps = here > 0 ? (V + ROWS - 1) / ROWS : 0, n0 = blockIdx.y * (8 * NT);
-    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (RING * STAGE);
+    const int steps = here > 0 ? (V - 1) / G_ROWS + 1 : 0, n0 = A.first_token;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * g_warp<P, NT, GB>;
+    float *const scale_of = (float *)(smem + warp * g_warp<P, NT, GB> + G_RING * STAGE);   // [2][row][group]
     const size_t row_bytes = (size_t)H / 2;
 
+    // fetching: this lane copies piece lane % 4 of rows lane / 4 + 8 i, and pieces of the tokens' rows
     int fs = slab, slot_f = 0;
-    const uint32_t put = ring + (lane >> 2) * 64 + ((t ^ (lane >> 4)) << 4), put8 = ring + (8 + (lane >> 2)) * 64 + ((t ^ (2 + (lane >> 4))) << 4);
-    const uint8_t *from = A.codes + (size_t)col / 2 + t * 16;
+    const uint32_t put = ring + (lane >> 2) * 64 + ((t ^ (lane >> 4)) << 4);
+    const uint8_t *const from = A.codes + (size_t)col / 2 + t * 16;
     auto fetch = [&]() {
         if (fs < steps) {
-            const int r = fs * ROWS + (lane >> 2);
+            const int r = fs * G_ROWS + (lane >> 2);
+            const uint32_t to = put + slot_f;
             if (t < here) {
-                cp16(put + slot_f * STAGE, from + min(r, V - 1) * row_bytes);
-                cp16(put8 + slot_f * STAGE, from + min(r + 8, V - 1) * row_bytes);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)                // (rows 8 on: the piece's place has another bit)
+                    cp16((to + i * 8 * 64) ^ (i & 1 ? 32 : 0), from + (size_t)min(r + 8 * i, V - 1) * row_bytes);
+            }
+#pragma unroll
+            for (int i = 0; i < 8 * NT * PIECES / 32; ++i) {
+                const int n = (i * 32 + lane) / PIECES, c = lane % PIECES, v = fs * G_ROWS + c * (16 / ESZ);
+                const int bytes = n0 + n < A.N ? max(0, min(16 / ESZ, V - v)) * ESZ : 0;
+                const char *at = (const char *)A.in + (bytes ? (int64_t)(n0 + n) * A.in_stride + v : 0) * ESZ;
+                cp16_part(ring + slot_f + G_CODES + n * (PIECES * 16) + ((c ^ (F32 ? (n & 1) << 2 : (n >> 1 & 1) << 1)) << 4), at, bytes);
             }
             fs += slabs;
         }
         cp_commit();
-        slot_f = slot_f + 1 == RING ? 0 : slot_f + 1;
+        slot_f = slot_f + STAGE == G_RING * STAGE ? 0 : slot_f + STAGE;
     };
 #pragma unroll
-    for (int i = 0; i < RING - 1; ++i) fetch();
+    for (int i = 0; i < G_RING - 1; ++i) fetch();
 
+    // the scales of row `lane` of a stage
+    Scales<GB> raw;
+    auto load_scales = [&](int s) {
+        const int r = s * G_ROWS + lane, i = col / (32 * GB);
+        if (r < V) raw.load(A.scales + (size_t)r * n_groups + i, n_groups - i, A.wide_scales);
+        else raw.clear();                                  // (zero times a gradient of zero)
+    };
     // a lane's words: rows 4t .. 4t + 3, word g / 2 of a block's piece (pieces of these rows are placed by t)
     const uint32_t get = ring + 4 * t * 64 + (g >> 1) * 4, pick = g & 1 ? HIGH : LOW;
-    const char *dy[NT];
-    bool has[NT];
+    const uint32_t get_d = ring + G_CODES + g * (PIECES * 16) + (F32 ? (t ^ (g & 1) << 2) << 4 : (g >> 1 & 1) << 5 | t << 3);
+    float acc[8][NT][4] = {}, eights[GROUPS][NT] = {};
+    int slot = 0, flip = 0;
+    if (slab < steps) load_scales(slab);
+    for (int s = slab; s < steps; s += slabs) {
 #pragma unroll
-    for (int q = 0; q < NT; ++q) {
-        has[q] = n0 + q * 8 + g < A.N;
-        dy[q] = (const char *)A.in + ((int64_t)(has[q] ? n0 + q * 8 + g : 0) * A.in_stride + 4 * t) * (P == 2 ? 2 : 4);
-    }
-    Scales<GB> sc[4], next_sc[4];
-    float d[NT][4], next_d[NT][4];
-    auto load = [&](int s) {
-        const int r = s * ROWS + 4 * t, i = col / (32 * GB);
-        const unsigned short *at = A.scales + (size_t)r * n_groups + i;
-        const bool whole = s * ROWS + ROWS <= V;
+        for (int i = 0; i < GROUPS; ++i) scale_of[(flip * G_ROWS + lane) * GROUPS + i] = raw.get(i);
+        if (s + slabs < steps) load_scales(s + slabs);
+        cp_wait<G_RING - 2>();
+        __syncwarp();
+        fetch();
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (whole || r + k < V) next_sc[k].load(at + (size_t)k * n_groups, n_groups - i, A.wide_scales);
-            else next_sc[k].clear();                       // (zero times a gradient of zero)
-        }
+        for (int half = 0; half < 2; ++half) {
+            float d[NT][4];
 #pragma unroll
-        for (int q = 0; q < NT; ++q) {
-            const char *p = dy[q] + (size_t)s * ROWS * (P == 2 ? 2 : 4);
-            if (!has[q]) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) next_d[q][k] = 0.f;
-            } else if (whole) {
-                if constexpr (P == 2) {
-                    const uint2 v = __ldg((const uint2 *)p);
-                    next_d[q][0] = od_bf16_lo(v.x); next_d[q][1] = od_bf16_hi(v.x);
-                    next_d[q][2] = od_bf16_lo(v.y); next_d[q][3] = od_bf16_hi(v.y);
+            for (int q = 0; q < NT; ++q) {
+                const uint32_t at = get_d + slot + q * 8 * (PIECES * 16);
+                if constexpr (F32) {
+                    const uint4 v = lds128(at ^ (half << 6));
+                    d[q][0] = __uint_as_float(v.x); d[q][1] = __uint_as_float(v.y);
+                    d[q][2] = __uint_as_float(v.z); d[q][3] = __uint_as_float(v.w);
                 } else {
-                    const float4 v = __ldg((const float4 *)p);
-                    next_d[q][0] = v.x; next_d[q][1] = v.y; next_d[q][2] = v.z; next_d[q][3] = v.w;
+                    uint2 v;
+                    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at ^ (half << 5)) : "memory");
+                    d[q][0] = od_bf16_lo(v.x); d[q][1] = od_bf16_hi(v.x); d[q][2] = od_bf16_lo(v.y); d[q][3] = od_bf16_hi(v.y);
                 }
+            }
+            const float *const sc = scale_of + (flip * G_ROWS + half * 16 + 4 * t) * GROUPS;
+            float e[4][GROUPS];
+            if constexpr (GROUPS == 1) {
+                const float4 v = *(const float4 *)sc;
+                e[0][0] = v.x; e[1][0] = v.y; e[2][0] = v.z; e[3][0] = v.w;
+            } else if constexpr (GROUPS == 2) {
+                const float4 v = *(const float4 *)sc, w = *(const float4 *)(sc + 4);
+                e[0][0] = v.x; e[0][1] = v.y; e[1][0] = v.z; e[1][1] = v.w;
+                e[2][0] = w.x; e[2][1] = w.y; e[3][0] = w.z; e[3][1] = w.w;
             } else {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    next_d[q][k] = 0.f;
-                    if (r + k < V) next_d[q][k] = P == 2 ? __uint_as_float((uint32_t)__ldg((const unsigned short *)p + k) << 16) : __ldg((const float *)p + k);
+                    const float4 v = *(const float4 *)(sc + 4 * k);
+                    e[k][0] = v.x; e[k][1] = v.y; e[k][2] = v.z; e[k][3] = v.w;
                 }
             }
-        }
-    };
-    float acc[8][NT][4] = {};
-    int slot = 0;
-    if (slab < steps) load(slab);
-    for (int s = slab; s < steps; s += slabs) {
+            const uint32_t rows = get + slot + half * 16 * 64;
+            uint32_t b[NT][2][P];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) sc[k] = next_sc[k];
+            for (int j = 0; j < 4; ++j) {
+                if (j >= here) break;
+                if (j % GB == 0) {
 #pragma unroll
-        for (int q = 0; q < NT; ++q)
+                    for (int q = 0; q < NT; ++q) {
+                        float z[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) d[q][k] = next_d[q][k];
-        if (s + slabs < steps) load(s + slabs);
-        cp_wait<RING - 2>();
-        __syncwarp();
-        fetch();
-        uint32_t b[NT][2][P];
+                        for (int k = 0; k < 4; ++k) z[k] = d[q][k] * e[k][j / GB] * UP;
+                        const float m = fmaxf(fmaxf(fabsf(z[0]), fabsf(z[1])), fmaxf(fabsf(z[2]), fabsf(z[3])));
+                        // (NaN is not in the maximum: its pieces are, and the sum is NaN)
+                        if (__any_sync(0xFFFFFFFFu, m == INFINITY)) {
+                            const unsigned lanes = __ballot_sync(0xFFFFFFFFu, m == INFINITY);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (j >= here) break;
-            if (j % GB == 0) {
+                            for (int k = 0; k < 4; ++k) {
+                                const float big = d[q][k] * e[k][j / GB];
+                                unsigned from_lanes = lanes & __ballot_sync(0xFFFFFFFFu, fabsf(z[k]) == INFINITY);
+                                if (fabsf(z[k]) == INFINITY) z[k] = 0.f;
+                                for (; from_lanes; from_lanes &= from_lanes - 1) {
+                                    const int src = __ffs(from_lanes) - 1, n = src >> 2, r = half * 16 + 4 * (src & 3) + k;
+                                    const float f = __shfl_sync(0xFFFFFFFFu, big, src) * (1.f / BACK);
 #pragma unroll
-                for (int q = 0; q < NT; ++q) {
-                    float z[4];
+                                    for (int i = 0; i < GB; ++i)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) z[k] = d[q][k] * sc[k].get(j / GB);
-                    const float m = fmaxf(fmaxf(fabsf(z[0]), fabsf(z[1])), fmaxf(fabsf(z[2]), fabsf(z[3])));
-                    const bool guard = __any_sync(0xFFFFFFFFu, m == INFINITY);
-                    pieces<P>(z[0], z[1], guard, b[q][0]);
-                    pieces<P>(z[2], z[3], guard, b[q][1]);
+                                        for (int a = 0; a < 2; ++a) {
+                                            if (j + i >= here) continue;
+                                            const uint32_t byte = smem[warp * g_warp<P, NT, GB> + slot + r * 64 + (((j + i) ^ (r >> 2 & 3)) << 4) + 2 * g + a];
+                                            const float lo = f * (float)((int)(byte & 15) - 8), hi = f * (float)((int)(byte >> 4) - 8) * 16.f;
+                                            if (2 * t == n) { acc[2 * (j + i) + a][q][0] += lo; acc[2 * (j + i) + a][q][2] += hi; }
+                                            if (2 * t + 1 == n) { acc[2 * (j + i) + a][q][1] += lo; acc[2 * (j + i) + a][q][3] += hi; }
+                                        }
+                                }
+                            }
+                        }
+                        pieces<P>(z[0], z[1], b[q][0]);
+                        pieces<P>(z[2], z[3], b[q][1]);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) eights[j / GB][q] = fmaf(z[k], 0x1p-126f * 0.0625f, eights[j / GB][q]);    // 8 times 2^-133
+                    }
                 }
+                const uint32_t at = rows + ((j ^ t) << 4);
+                const uint32_t w01 = halves(lds32(at), lds32(at + 64), pick), w23 = halves(lds32(at + 128), lds32(at + 192), pick);
+                const uint32_t v01 = w01 >> 8, v23 = w23 >> 8;
+                const uint32_t a0[4] = {w01 & CODE, w01 & CODE16, w23 & CODE, w23 & CODE16};       // (rows 8 on are 16 times as much)
+                const uint32_t a1[4] = {v01 & CODE, v01 & CODE16, v23 & CODE, v23 & CODE16};
+#pragma unroll
+                for (int q = 0; q < NT; ++q)
+#pragma unroll
+                    for (int p = 0; p < P; ++p) {
+                        mma(acc[2 * j][q], a0, b[q][0][p], b[q][1][p]);
+                        mma(acc[2 * j + 1][q], a1, b[q][0][p], b[q][1][p]);
+                    }
             }
-            const uint32_t at = get + slot * STAGE + ((j ^ t) << 4);
-            const uint32_t w01 = halves(lds32(at), lds32(at + 64), pick), w23 = halves(lds32(at + 128), lds32(at + 192), pick);
-            const uint32_t a0[4] = {unpack<0>(w01, A.bf16_128), unpack<1>(w01, A.bf16_128), unpack<0>(w23, A.bf16_128), unpack<1>(w23, A.bf16_128)};
-            const uint32_t a1[4] = {unpack<2>(w01, A.bf16_128), unpack<3>(w01, A.bf16_128), unpack<2>(w23, A.bf16_128), unpack<3>(w23, A.bf16_128)};
-#pragma unroll
-            for (int q = 0; q < NT; ++q)
-#pragma unroll
-                for (int p = 0; p < P; ++p) {
-                    mma(acc[2 * j][q], a0, b[q][0][p], b[q][1][p]);
-                    mma(acc[2 * j + 1][q], a1, b[q][0][p], b[q][1][p]);
-                }
         }
-        slot = slot + 1 == RING ? 0 : slot + 1;
+        slot = slot + STAGE == G_RING * STAGE ? 0 : slot + STAGE;
+        flip ^= 1;
     }
     cp_wait<0>();
     __syncthreads();                                       // the rings are free
 
     // [warp][token][column]; the warps on the same columns are summed into the first of them
     constexpr int PART = 8 * NT * COLS;                    // numbers of a warp
-    float *part = (float *)smem;
+    float *const part = (float *)smem;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int i = 0; i < GROUPS; ++i)
 #pragma unroll
-        for (int a = 0; a < 2; ++a)
+        for (int q = 0; q < NT; ++q) {
+            float v = eights[i][q];
+            v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
+            v += __shfl_xor_sync(0xFFFFFFFFu, v, 2);       // of token g
+            const float e[2] = {__shfl_sync(0xFFFFFFFFu, v, 8 * t), __shfl_sync(0xFFFFFFFFu, v, 8 * t + 4)};
 #pragma unroll
-            for (int q = 0; q < NT; ++q)
+            for (int j = i * GB; j < (i + 1) * GB; ++j)
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
-                    *(float2 *)(part + warp * PART + (q * 8 + 2 * t + k) * COLS + 32 * j + 4 * g + 2 * a) =
-                        make_float2(acc[2 * j + a][q][k], acc[2 * j + a][q][k + 2]);
+                for (int a = 0; a < 2; ++a)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const float *c = acc[2 * j + a][q];
+                        *(float2 *)(part + warp * PART + (q * 8 + 2 * t + k) * COLS + 32 * j + 4 * g + 2 * a) =
+                            make_float2((c[k] - e[k]) * BACK, (c[k + 2] * 0.0625f - e[k]) * BACK);
+                    }
+        }
     __syncthreads();
-    const int n_sums = cw * PART;
-    for (int i = threadIdx.x; i < n_sums; i += THREADS) {
+    for (int i = threadIdx.x; i < cw * PART; i += THREADS) {
         float v = part[i];
         for (int w = cw; w < WARPS; w += cw) v += part[w * PART + i];
-        part[i] = v;
-    }
-    __syncthreads();
-    if (split > 1) { od_cluster_arrive(); od_cluster_wait(); }
-    // and the blocks of the cluster, each a share of the columns
-    for (int i = (int)((int64_t)n_sums * rank / split) + threadIdx.x; i < (int)((int64_t)n_sums * (rank + 1) / split); i += THREADS) {
         const int n = n0 + i % PART / COLS, h = (tile * cw + i / PART) * COLS + i % COLS;
-        float v = 0.f;
-        for (int r = 0; r < split; ++r) v += split > 1 ? lds_cluster(od_cluster_address(part + i, r)) : part[i];
-        if (n < A.N && h < H) store(A, n, h, v);
+        if (split > 1) A.parts[(size_t)blockIdx.x * (cw * PART) + i] = v;
+        else if (n < A.N && h < H) store(A, n, h, v);
     }
-    if (split > 1) { od_cluster_arrive(); od_cluster_wait(); }
 }
 
-constexpr int ring_bytes = WARPS * RING * STAGE, wide_bytes = F_WARPS * WIDE_RING * WIDE_STAGE;
+// the blocks on the same columns: [tile][split][warp side by side][token][column]
+__global__ void od_q4_join_kernel(const Q4Args A, int tokens)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int i = blockIdx.x * blockDim.x + threadIdx.x, n = i / A.H, h = i % A.H;
+    if (n >= tokens || A.first_token + n >= A.N) return;
+    const int size = A.col_warps * tokens * COLS, tile = h / (A.col_warps * COLS);
+    const float *p = A.parts + (size_t)tile * A.split * size + (h / COLS % A.col_warps * tokens + n) * COLS + h % COLS;
+    float v = 0.f;
+#pragma unroll 8
+    for (int k = 0; k < A.split; ++k) v += p[(size_t)k * size];
+    store(A, A.first_token + n, h, v);
+}
+
+constexpr int wide_bytes = F_WARPS * WIDE_RING * WIDE_STAGE;
 template <int NT> constexpr int part_bytes = F_WARPS * NT * 512;
-template <int NT> constexpr int grad_bytes = WARPS * 8 * NT * COLS * 4 > ring_bytes ? WARPS * 8 * NT * COLS * 4 : ring_bytes;
+template <int P, int NT, int GB> constexpr int grad_bytes = WARPS * (g_warp<P, NT, GB> > 8 * NT * COLS * 4 ? g_warp<P, NT, GB> : 8 * NT * COLS * 4);
 
 typedef void (*Kernel)(Q4Args);
 struct Variant { Kernel kernel; int smem, tokens, threads = F_THREADS; };
@@ -638,8 +678,8 @@ Variant forward_of(bool f32, int N, int32_t H)
 template <int GB>
 Variant backward_of(bool f32, int N)
 {
-    if (f32) return N <= 8 ? Variant{od_q4_grad_kernel<3, 1, GB>, grad_bytes<1>, 8, THREADS} : Variant{od_q4_grad_kernel<3, 2, GB>, grad_bytes<2>, 16, THREADS};
-    return N <= 8 ? Variant{od_q4_grad_kernel<2, 1, GB>, grad_bytes<1>, 8, THREADS} : Variant{od_q4_grad_kernel<2, 2, GB>, grad_bytes<2>, 16, THREADS};
+    if (f32) return N <= 8 ? Variant{od_q4_grad_kernel<3, 1, GB>, grad_bytes<3, 1, GB>, 8, THREADS} : Variant{od_q4_grad_kernel<3, 2, GB>, grad_bytes<3, 2, GB>, 16, THREADS};
+    return N <= 8 ? Variant{od_q4_grad_kernel<2, 1, GB>, grad_bytes<2, 1, GB>, 8, THREADS} : Variant{od_q4_grad_kernel<2, 2, GB>, grad_bytes<2, 2, GB>, 16, THREADS};
 }
 Variant variant(bool backward, int32_t G, bool f32, int N, int32_t H)
 {
@@ -647,22 +687,22 @@ Variant variant(bool backward, int32_t G, bool f32, int N, int32_t H)
     return G == 32 ? forward_of<1>(f32, N, H) : G == 64 ? forward_of<2>(f32, N, H) : forward_of<4>(f32, N, H);
 }
 
-void configure(cudaLaunchConfig_t &cfg, cudaLaunchAttribute (&attr)[2], const Variant &v, unsigned blocks, unsigned tiles, unsigned cluster)
+template <typename K, typename... A>
+cudaError_t launch(K kernel, dim3 grid, int threads, int smem, bool pdl, cudaStream_t s, A... args)
 {
-    cfg = {};
-    cfg.gridDim = dim3(blocks, tiles); cfg.blockDim = dim3(v.threads);
-    cfg.dynamicSmemBytes = v.smem;
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr; cfg.numAttrs = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid; cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem; cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = pdl ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 }  // namespace
 
-// the kernels' limits; clusters[0 / 1][n]: clusters of n blocks that are resident at a time, up to 8 / more tokens
-cudaError_t od_q4_prepare_device(int32_t (*clusters)[OD_Q4_MAX_SPLIT + 1])
+cudaError_t od_q4_prepare_device()
 {
     for (int backward = 0; backward < 2; ++backward)
         for (int32_t G = 32; G <= 128; G *= 2)
@@ -670,35 +710,21 @@ cudaError_t od_q4_prepare_device(int32_t (*clusters)[OD_Q4_MAX_SPLIT + 1])
                 for (int N = 8; N <= 64; N *= 2) {         // (64: none in shared memory)
                     const Variant v = variant(backward, G, f32, N, N == 64 ? 65536 : 128);
                     cudaError_t e = cudaFuncSetAttribute((const void *)v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST);
-                    if (e == cudaSuccess && backward) e = cudaFuncSetAttribute((const void *)v.kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
                     if (e != cudaSuccess) return e;
                 }
-    for (int wide = 0; wide < 2; ++wide)
-        for (int n = 1; n <= MAX_SPLIT; ++n) {
-            cudaLaunchConfig_t cfg;
-            cudaLaunchAttribute attr[2];
-            const Variant v = variant(true, 32, true, wide ? 16 : 8, 128);
-            configure(cfg, attr, v, (unsigned)n, 1, (unsigned)n);
-            int here = 0;
-            if (cudaOccupancyMaxActiveClusters(&here, (const void *)v.kernel, &cfg) != cudaSuccess) {
-                cudaGetLastError();
-                here = 0;
-            }
-            clusters[wide][n] = here;
-        }
     return cudaSuccess;
 }
 
 cudaError_t od_launch_q4(const od_ctx *c, bool backward, int32_t N, int32_t V, int32_t H, int32_t G, const void *a, int32_t a_dtype,
                          int64_t as, const void *codes, const void *scales, void *b, int32_t b_dtype, int64_t bs, cudaStream_t s)
 {
-    const Variant v = variant(backward, G, a_dtype == OD_F32, N, H);
-    Q4Args args = {a, as, (const uint8_t *)codes, (const unsigned short *)scales, b, bs, N, V, H, a_dtype == OD_F32, b_dtype == OD_F32,
-                   H % COLS == 0 && ((uintptr_t)scales & 7u) == 0, 0x43004300u, 1, 1, 1};
-    unsigned blocks;
+    const bool f32 = a_dtype == OD_F32, pdl = c->opt_pdl != 0;
+    const int32_t sms = c->sm_count;
+    Q4Args args = {a, as, (const uint8_t *)codes, (const unsigned short *)scales, b, bs, N, V, H, f32, b_dtype == OD_F32,
+                   H % COLS == 0 && ((uintptr_t)scales & 7u) == 0, 1, 1, 1, 0, c->d_q4_parts};
     if (!backward) {
-        const int64_t units = ((int64_t)V + ROWS - 1) / ROWS;
-        blocks = (unsigned)(units < c->sm_count ? units : c->sm_count);
+        const Variant v = variant(false, G, f32, N, H);
+        const int64_t units = ((int64_t)V + ROWS - 1) / ROWS, blocks = units < sms ? units : sms;
         // Warps to the same 16 rows (1, 2, 4): the fewest stages in a row of one warp, of equal ones the fewest warps
         const int64_t each = (units + blocks - 1) / blocks, stages = (H + 32 * WIDE - 1) / (32 * WIDE);
         int64_t best = INT64_MAX;
@@ -706,26 +732,28 @@ cudaError_t od_launch_q4(const od_ctx *c, bool backward, int32_t N, int32_t V, i
             const int64_t cost = (each * ks + F_WARPS - 1) / F_WARPS * ((stages + ks - 1) / ks);
             if (cost < best) { best = cost; args.k_split = ks; }
         }
-    } else {
-        // How many warps side by side (4, 2, 1) and blocks to a cluster (any number that the device holds): the fewest
-        // rounds of clusters times rows of a warp; of equal ones the widest rows.
-        const int32_t *resident = c->q4_clusters[v.tokens > 8];
-        int64_t best = INT64_MAX;
-        int32_t tiles_of = 1;
-        for (int32_t cw = 4; cw >= 1; cw /= 2)
-            for (int32_t n = 1; n <= MAX_SPLIT; ++n) {
-                if (resident[n] < 1) continue;
-                const int32_t tiles = (H + cw * COLS - 1) / (cw * COLS);
-                const int64_t rounds = (tiles + resident[n] - 1) / resident[n];
-                const int64_t cost = rounds * ((V + ROWS - 1) / ROWS + n * (WARPS / cw) - 1) / (n * (WARPS / cw));
-                if (cost < best) { best = cost; args.col_warps = cw; args.split = n; tiles_of = tiles; }
-            }
-        blocks = (unsigned)(tiles_of * args.split);
+        return launch(v.kernel, dim3((unsigned)blocks, (unsigned)((N + v.tokens - 1) / v.tokens)), F_THREADS, v.smem, pdl, s, args);
     }
-    cudaLaunchConfig_t cfg;
-    cudaLaunchAttribute attr[2];
-    configure(cfg, attr, v, blocks, (unsigned)((N + v.tokens - 1) / v.tokens), (unsigned)args.split);
-    cfg.stream = s;
-    cfg.numAttrs = c->opt_pdl ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, v.kernel, args);
+    // 16 tokens at a time, then 8: the scratch is for one time
+    for (int32_t n = 0; n < N;) {
+        const Variant v = variant(true, G, f32, N - n, H);
+        // Warps side by side (4, 2, 1) and blocks on the same columns (as many as there are multiprocessors for): the fewest
+        // stages of a warp; of equal ones the widest rows.
+        const int64_t steps = ((int64_t)V + G_ROWS - 1) / G_ROWS;
+        int64_t best = INT64_MAX, blocks = 0;
+        for (int32_t cw = 4 * 8 / v.tokens; cw >= 1; cw /= 2) {
+            const int64_t tiles = (H + cw * COLS - 1) / (cw * COLS), deep = WARPS / cw;
+            int64_t split = sms / tiles < 1 ? 1 : sms / tiles;
+            if (split > (steps + deep - 1) / deep) split = (steps + deep - 1) / deep;
+            const int64_t cost = (tiles * split + sms - 1) / sms * ((steps + split * deep - 1) / (split * deep));
+            if (cost < best) { best = cost; blocks = tiles * split; args.col_warps = cw; args.split = (int32_t)split; }
+        }
+        args.first_token = n;
+        cudaError_t e = launch(v.kernel, dim3((unsigned)blocks), THREADS, v.smem, pdl, s, args);
+        if (e == cudaSuccess && args.split > 1)
+            e = launch(od_q4_join_kernel, dim3((unsigned)(((int64_t)v.tokens * H + 255) / 256)), 256, 0, pdl, s, args, v.tokens);
+        if (e != cudaSuccess) return e;
+        n += v.tokens;
+    }
+    return cudaSuccess;
 }
