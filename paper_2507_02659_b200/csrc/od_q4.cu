@@ -423,8 +423,7 @@ __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
 
 // ---- backward: 128 columns to a warp, every so many-th 32 rows ----------------------------------
 //
-// Rows are summed over: two of them are the pair of an operand, four columns in a row are a half word, so a block of 32
-// columns is the sixteen rows of two fragments. A lane reads the word that its half is in of four rows. The tokens' side is
+// Rows are summed over: two of them are the pair of an operand, four columns in a row are a half word. The tokens' side is
 // made anew for each group: gradient times scale, in pieces. It is scaled by 2^110 for what the codes are as bf16 numbers;
 // what is too large for that (and infinities and NaN) is added to the sums on its own. The 8 of a code is taken off at the
 // end: sums of gradient times scale, of which a lane has those of its rows.
@@ -497,8 +496,10 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
         if (r < V) raw.load(A.scales + (size_t)r * n_groups + i, n_groups - i, A.wide_scales);
         else raw.clear();                                  // (zero times a gradient of zero)
     };
-    // a lane's words: rows 4t .. 4t + 3, word g / 2 of a block's piece (pieces of these rows are placed by t)
-    const uint32_t get = ring + 4 * t * 64 + (g >> 1) * 4, pick = g & 1 ? HIGH : LOW;
+    // A lane's words: rows 4t .. 4t + 3; of a group of 64 or more word g of two blocks, of one of 32 a half of word g / 2 of
+    // a block. (Pieces of these rows are placed by t.)
+    constexpr bool PAIRS = GB > 1;
+    const uint32_t get = ring + 4 * t * 64 + (PAIRS ? g & 3 : g >> 1) * 4, pick = g & 1 ? HIGH : LOW;
     const uint32_t get_d = ring + G_CODES + g * (PIECES * 16) + (F32 ? (t ^ (g & 1) << 2) << 4 : (g >> 1 & 1) << 5 | t << 3);
     float acc[8][NT][4] = {}, eights[GROUPS][NT] = {};
     int slot = 0, flip = 0;
@@ -510,93 +511,108 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
         cp_wait<G_RING - 2>();
         __syncwarp();
         fetch();
+        // both halves of the rows side by side, for what can run at the same time
+        float d[2][NT][4], e[2][4][GROUPS];
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            float d[NT][4];
 #pragma unroll
             for (int q = 0; q < NT; ++q) {
                 const uint32_t at = get_d + slot + q * 8 * (PIECES * 16);
                 if constexpr (F32) {
                     const uint4 v = lds128(at ^ (half << 6));
-                    d[q][0] = __uint_as_float(v.x); d[q][1] = __uint_as_float(v.y);
-                    d[q][2] = __uint_as_float(v.z); d[q][3] = __uint_as_float(v.w);
+                    d[half][q][0] = __uint_as_float(v.x); d[half][q][1] = __uint_as_float(v.y);
+                    d[half][q][2] = __uint_as_float(v.z); d[half][q][3] = __uint_as_float(v.w);
                 } else {
                     uint2 v;
                     asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at ^ (half << 5)) : "memory");
-                    d[q][0] = od_bf16_lo(v.x); d[q][1] = od_bf16_hi(v.x); d[q][2] = od_bf16_lo(v.y); d[q][3] = od_bf16_hi(v.y);
+                    d[half][q][0] = od_bf16_lo(v.x); d[half][q][1] = od_bf16_hi(v.x);
+                    d[half][q][2] = od_bf16_lo(v.y); d[half][q][3] = od_bf16_hi(v.y);
                 }
             }
-            const float *const sc = scale_of + (flip * G_ROWS + half * 16 + 4 * t) * GROUPS;
-            float e[4][GROUPS];
-            if constexpr (GROUPS == 1) {
-                const float4 v = *(const float4 *)sc;
-                e[0][0] = v.x; e[1][0] = v.y; e[2][0] = v.z; e[3][0] = v.w;
-            } else if constexpr (GROUPS == 2) {
-                const float4 v = *(const float4 *)sc, w = *(const float4 *)(sc + 4);
-                e[0][0] = v.x; e[0][1] = v.y; e[1][0] = v.z; e[1][1] = v.w;
-                e[2][0] = w.x; e[2][1] = w.y; e[3][0] = w.z; e[3][1] = w.w;
-            } else {
+            float flat[4 * GROUPS];                        // [row][group]
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float4 v = *(const float4 *)(sc + 4 * k);
-                    e[k][0] = v.x; e[k][1] = v.y; e[k][2] = v.z; e[k][3] = v.w;
+            for (int k = 0; k < GROUPS; ++k)
+                *(float4 *)(flat + 4 * k) = *(const float4 *)(scale_of + (flip * G_ROWS + half * 16 + 4 * t) * GROUPS + 4 * k);
+#pragma unroll
+            for (int k = 0; k < 4 * GROUPS; ++k) e[half][k / GROUPS][k % GROUPS] = flat[k];
+        }
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i) {
+            if (i * GB >= here) break;
+            float z[2][NT][4], m = 0.f;
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int q = 0; q < NT; ++q) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        z[half][q][k] = d[half][q][k] * e[half][k][i] * UP;
+                        m = fmaxf(m, fabsf(z[half][q][k]));
+                    }
                 }
-            }
-            const uint32_t rows = get + slot + half * 16 * 64;
-            uint32_t b[NT][2][P];
+            // (NaN is not in the maximum: its pieces are, and the sum is NaN)
+            if (__any_sync(0xFFFFFFFFu, m == INFINITY)) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (j >= here) break;
-                if (j % GB == 0) {
+                for (int half = 0; half < 2; ++half)
 #pragma unroll
-                    for (int q = 0; q < NT; ++q) {
-                        float z[4];
+                    for (int q = 0; q < NT; ++q)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) z[k] = d[q][k] * e[k][j / GB] * UP;
-                        const float m = fmaxf(fmaxf(fabsf(z[0]), fabsf(z[1])), fmaxf(fabsf(z[2]), fabsf(z[3])));
-                        // (NaN is not in the maximum: its pieces are, and the sum is NaN)
-                        if (__any_sync(0xFFFFFFFFu, m == INFINITY)) {
-                            const unsigned lanes = __ballot_sync(0xFFFFFFFFu, m == INFINITY);
+                        for (int k = 0; k < 4; ++k) {
+                            const bool large = fabsf(z[half][q][k]) == INFINITY;
+                            const float big = d[half][q][k] * e[half][k][i] * (1.f / BACK);
+                            if (large) z[half][q][k] = 0.f;
+                            for (unsigned lanes = __ballot_sync(0xFFFFFFFFu, large); lanes; lanes &= lanes - 1) {
+                                const int src = __ffs(lanes) - 1, n = src >> 2, r = half * 16 + 4 * (src & 3) + k;
+                                const float f = __shfl_sync(0xFFFFFFFFu, big, src);
+                                const unsigned char *const row = smem + warp * g_warp<P, NT, GB> + slot + r * 64;
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                const float big = d[q][k] * e[k][j / GB];
-                                unsigned from_lanes = lanes & __ballot_sync(0xFFFFFFFFu, fabsf(z[k]) == INFINITY);
-                                if (fabsf(z[k]) == INFINITY) z[k] = 0.f;
-                                for (; from_lanes; from_lanes &= from_lanes - 1) {
-                                    const int src = __ffs(from_lanes) - 1, n = src >> 2, r = half * 16 + 4 * (src & 3) + k;
-                                    const float f = __shfl_sync(0xFFFFFFFFu, big, src) * (1.f / BACK);
-#pragma unroll
-                                    for (int i = 0; i < GB; ++i)
-#pragma unroll
-                                        for (int a = 0; a < 2; ++a) {
-                                            if (j + i >= here) continue;
-                                            const uint32_t byte = smem[warp * g_warp<P, NT, GB> + slot + r * 64 + (((j + i) ^ (r >> 2 & 3)) << 4) + 2 * g + a];
-                                            const float lo = f * (float)((int)(byte & 15) - 8), hi = f * (float)((int)(byte >> 4) - 8) * 16.f;
-                                            if (2 * t == n) { acc[2 * (j + i) + a][q][0] += lo; acc[2 * (j + i) + a][q][2] += hi; }
-                                            if (2 * t + 1 == n) { acc[2 * (j + i) + a][q][1] += lo; acc[2 * (j + i) + a][q][3] += hi; }
-                                        }
+                                for (int c = 2 * i * GB; c < 2 * (i + 1) * GB; ++c) {
+                                    // the byte of a lane's two columns of sum c
+                                    const int at = PAIRS ? c / 4 * 32 + 4 * g + c % 4 : c / 2 * 16 + 2 * g + c % 2;
+                                    const uint32_t byte = row[((at >> 4 ^ (r >> 2 & 3)) << 4) + (at & 15)];
+                                    const float lo = f * (float)((int)(byte & 15) - 8), hi = f * (float)((int)(byte >> 4) - 8) * 16.f;
+                                    if (2 * t == n) { acc[c][q][0] += lo; acc[c][q][2] += hi; }
+                                    if (2 * t + 1 == n) { acc[c][q][1] += lo; acc[c][q][3] += hi; }
                                 }
                             }
                         }
-                        pieces<P>(z[0], z[1], b[q][0]);
-                        pieces<P>(z[2], z[3], b[q][1]);
+            }
+            uint32_t b[2][NT][2][P];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) eights[j / GB][q] = fmaf(z[k], 0x1p-126f * 0.0625f, eights[j / GB][q]);    // 8 times 2^-133
-                    }
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int q = 0; q < NT; ++q) {
+                    pieces<P>(z[half][q][0], z[half][q][1], b[half][q][0]);
+                    pieces<P>(z[half][q][2], z[half][q][3], b[half][q][1]);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) eights[i][q] = fmaf(z[half][q][k], 0x1p-126f * 0.0625f, eights[i][q]);     // 8 times 2^-133
                 }
-                const uint32_t at = rows + ((j ^ t) << 4);
-                const uint32_t w01 = halves(lds32(at), lds32(at + 64), pick), w23 = halves(lds32(at + 128), lds32(at + 192), pick);
+            // four codes of a lane in each of four rows: two columns of two sums
+            auto product = [&](uint32_t w01, uint32_t w23, int half, int c) {
                 const uint32_t v01 = w01 >> 8, v23 = w23 >> 8;
                 const uint32_t a0[4] = {w01 & CODE, w01 & CODE16, w23 & CODE, w23 & CODE16};       // (rows 8 on are 16 times as much)
                 const uint32_t a1[4] = {v01 & CODE, v01 & CODE16, v23 & CODE, v23 & CODE16};
 #pragma unroll
-                for (int q = 0; q < NT; ++q)
+                for (int p = 0; p < P; ++p)
 #pragma unroll
-                    for (int p = 0; p < P; ++p) {
-                        mma(acc[2 * j][q], a0, b[q][0][p], b[q][1][p]);
-                        mma(acc[2 * j + 1][q], a1, b[q][0][p], b[q][1][p]);
+                    for (int q = 0; q < NT; ++q) {
+                        mma(acc[c][q], a0, b[half][q][0][p], b[half][q][1][p]);
+                        mma(acc[c + 1][q], a1, b[half][q][0][p], b[half][q][1][p]);
                     }
-            }
+            };
+#pragma unroll
+            for (int j = i * GB; j < (i + 1) * GB; j += PAIRS ? 2 : 1)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t at = get + slot + half * 16 * 64 + ((PAIRS ? (j + (g >> 2)) ^ t : j ^ t) << 4);
+                    const uint32_t w0 = lds32(at), w1 = lds32(at + 64), w2 = lds32(at + 128), w3 = lds32(at + 192);
+                    if constexpr (PAIRS) {
+                        product(halves(w0, w1, LOW), halves(w2, w3, LOW), half, 2 * j);
+                        product(halves(w0, w1, HIGH), halves(w2, w3, HIGH), half, 2 * j + 2);
+                    } else {
+                        product(halves(w0, w1, pick), halves(w2, w3, pick), half, 2 * j);
+                    }
+                }
         }
         slot = slot + STAGE == G_RING * STAGE ? 0 : slot + STAGE;
         flip ^= 1;
@@ -616,15 +632,13 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
             v += __shfl_xor_sync(0xFFFFFFFFu, v, 2);       // of token g
             const float e[2] = {__shfl_sync(0xFFFFFFFFu, v, 8 * t), __shfl_sync(0xFFFFFFFFu, v, 8 * t + 4)};
 #pragma unroll
-            for (int j = i * GB; j < (i + 1) * GB; ++j)
+            for (int c = 2 * i * GB; c < 2 * (i + 1) * GB; ++c)
 #pragma unroll
-                for (int a = 0; a < 2; ++a)
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const float *c = acc[2 * j + a][q];
-                        *(float2 *)(part + warp * PART + (q * 8 + 2 * t + k) * COLS + 32 * j + 4 * g + 2 * a) =
-                            make_float2((c[k] - e[k]) * BACK, (c[k + 2] * 0.0625f - e[k]) * BACK);
-                    }
+                for (int k = 0; k < 2; ++k) {
+                    const int column = PAIRS ? c / 4 * 64 + 8 * g + c % 4 * 2 : c / 2 * 32 + 4 * g + c % 2 * 2;
+                    *(float2 *)(part + warp * PART + (q * 8 + 2 * t + k) * COLS + column) =
+                        make_float2((acc[c][q][k] - e[k]) * BACK, (acc[c][q][k + 2] * 0.0625f - e[k]) * BACK);
+                }
         }
     __syncthreads();
     for (int i = threadIdx.x; i < cw * PART; i += THREADS) {
