@@ -11,9 +11,9 @@
 // Forward: one pass. A block of 256 threads (or a cluster of them: one contiguous slice of the row to each) keeps, per
 // thread, the maximum, the sum of e and the sum of e (x - M), raised to a new maximum once per four 16-byte loads.
 // The alternatives cost next to nothing in that pass: the largest logits of 32 groups of eight threads are 32 different
-// elements, so the n-th largest of them is a bound that at least n elements of the slice reach and few more do; only
-// the threads whose own maximum reaches it look at their elements again (from L2), and what reaches the bound is
-// ranked by counting.
+// elements, so the n-th largest of them is a bound that at least n elements of the slice reach and few more do. Threads leave
+// the maximum of every four loads in shared memory: only loads whose maximum reaches the bound are looked at again (from L2,
+// all of them at once), and what reaches the bound is ranked by counting.
 //
 // Backward: elementwise, one read and one write; the given token and the alternatives are written over the dense
 // values of their chunk behind a block barrier.
@@ -29,10 +29,13 @@ constexpr int GROUPS = THREADS / 8;                        // of eight threads
 constexpr int U = 4;                                       // 16-byte loads of a thread in flight
 constexpr int MAX_SPLIT = 8;                               // blocks of a row (a portable cluster)
 constexpr int CAP = 512;                                   // candidates that are ranked by counting
+constexpr int SLOTS = 32;                                  // maxima that a thread leaves
+constexpr int AGAIN = 256;                                 // of them that are looked at again
 constexpr float LEAST = -150.f;                            // exp2 of it is zero
 constexpr float LN2 = 0.69314718055994531f, LOG2E = 1.4426950408889634f;
 static_assert(GROUPS == 32, "a group to each lane");
-static_assert(WARPS * OD_MAX_TOP <= CAP && MAX_SPLIT * OD_MAX_TOP <= CAP, "a list from every warp, or block, fits");
+static_assert(MAX_SPLIT * OD_MAX_TOP <= THREADS, "a thread to each alternative of the blocks");
+static_assert(WARPS * OD_MAX_TOP <= CAP, "a list from every warp fits");
 
 struct ScoreArgs {
     const char *logits;
@@ -115,7 +118,7 @@ __device__ __forceinline__ void absorb_pair(uint64_t &s2, uint64_t &a2, float lo
 }
 
 template <int DTYPE>
-__device__ __forceinline__ void absorb(Sums &t, const uint4 (&x)[U], float scale)
+__device__ __forceinline__ float absorb(Sums &t, const uint4 (&x)[U], float scale)
 {
     float gm;
     if (DTYPE == OD_BF16) {
@@ -146,19 +149,42 @@ __device__ __forceinline__ void absorb(Sums &t, const uint4 (&x)[U], float scale
     t.s += p + q;
     f2_unpack(f2_add(a0, a1), p, q);
     t.a += p + q;
+    return gm;
 }
 
-// the order of the alternatives: by logit, then by the lower id
-__device__ __forceinline__ bool before(float v, int i, float w, int j) { return v > w || (v == w && i < j); }
-
-// Sorted list of the best in a warp's lanes, lane 0 first; the same (v, i) in every lane goes in at its place.
-__device__ __forceinline__ void list_insert(float &lv, int &li, float v, int i, int lane)
+// The order of the alternatives, by logit and then by the lower id, as one number: the larger comes first. 0 is none.
+typedef unsigned long long Key;
+__device__ __forceinline__ Key key_of(float v, int i)
 {
-    const int at = __popc(__ballot_sync(0xFFFFFFFFu, before(lv, li, v, i)));
-    const float uv = __shfl_up_sync(0xFFFFFFFFu, lv, 1);
-    const int ui = __shfl_up_sync(0xFFFFFFFFu, li, 1);
-    if (lane > at) { lv = uv; li = ui; }
-    if (lane == at) { lv = v; li = i; }
+    const uint32_t b = __float_as_uint(v + 0.f);           // (-0 is 0)
+    return (Key)(b ^ ((int32_t)b < 0 ? 0xFFFFFFFFu : 0x80000000u)) << 32 | (0xFFFFFFFFu - (uint32_t)i);
+}
+__device__ __forceinline__ float logit_of(Key k)
+{
+    const uint32_t o = (uint32_t)(k >> 32);
+    return __uint_as_float(o ^ ((int32_t)o < 0 ? 0x80000000u : 0xFFFFFFFFu));
+}
+__device__ __forceinline__ int id_of(Key k) { return (int)(0xFFFFFFFFu - (uint32_t)k); }
+
+// how many of count keys (a multiple of four, a 16-byte aligned place in shared memory) come in front of k
+__device__ __forceinline__ int keys_in_front(const Key *keys, int count, Key k)
+{
+    int rank = 0;
+#pragma unroll 2
+    for (int i = 0; i < count; i += 4) {
+        const ulonglong2 a = *(const ulonglong2 *)(keys + i), b = *(const ulonglong2 *)(keys + i + 2);
+        rank += (a.x > k) + (a.y > k) + (b.x > k) + (b.y > k);
+    }
+    return rank;
+}
+
+// Sorted list of the best in a warp's lanes, lane 0 first; the same k in every lane goes in at its place.
+__device__ __forceinline__ void list_insert(Key &l, Key k, int lane)
+{
+    const int at = __popc(__ballot_sync(0xFFFFFFFFu, l > k));
+    const Key up = __shfl_up_sync(0xFFFFFFFFu, l, 1);
+    if (lane > at) l = up;
+    if (lane == at) l = k;
 }
 
 __device__ __forceinline__ void store_cluster(float *p, uint32_t rank, float v)
@@ -168,6 +194,10 @@ __device__ __forceinline__ void store_cluster(float *p, uint32_t rank, float v)
 __device__ __forceinline__ void store_cluster(int *p, uint32_t rank, int v)
 {
     asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(od_cluster_address(p, rank)), "r"(v) : "memory");
+}
+__device__ __forceinline__ void store_cluster(Key *p, uint32_t rank, Key v)
+{
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(od_cluster_address(p, rank)), "l"(v) : "memory");
 }
 
 // over a warp: the largest c, and the sums at it
@@ -193,8 +223,11 @@ __global__ void __launch_bounds__(THREADS, 4) od_score_kernel(const ScoreArgs A)
 {
     __shared__ float group_max[GROUPS];
     __shared__ Sums warp_sums[WARPS], block_sums[MAX_SPLIT];
-    __shared__ float cand_v[TOP ? CAP : 1], list_v[TOP ? OD_MAX_TOP : 1], best_v[TOP ? MAX_SPLIT * OD_MAX_TOP : 1];
-    __shared__ int cand_i[TOP ? CAP : 1], list_i[TOP ? OD_MAX_TOP : 1], best_i[TOP ? MAX_SPLIT * OD_MAX_TOP : 1];
+    // candidates, and the best of all blocks of the row; maxima, and those that reach the bound (slot << 8 | thread)
+    __shared__ __align__(16) Key cand[TOP ? CAP : 1], best[TOP ? MAX_SPLIT * OD_MAX_TOP : 1];
+    __shared__ float maxima[TOP ? SLOTS : 1][THREADS];
+    __shared__ unsigned short again[TOP ? AGAIN : 1];
+    __shared__ int n_again, filled_of[MAX_SPLIT];          // (alternatives of each block)
     __shared__ int n_cand;
 
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -222,7 +255,11 @@ __global__ void __launch_bounds__(THREADS, 4) od_score_kernel(const ScoreArgs A)
         }
         return;
     }
-    od_cluster_arrive_relaxed();                           // waited for before this block writes into another
+    if (TOP) {
+        for (int i = tid; i < CAP; i += THREADS) cand[i] = 0;
+        if (tid == 0) n_cand = n_again = 0;
+    }
+    if (split > 1) od_cluster_arrive_relaxed();            // waited for before this block writes into another
     const float scale = LOG2E / T;
     float x_t = 0.f;                                       // requested early, by the thread that uses it
     if (tid == 0 && part == 0 && id >= 0 && id < V) x_t = od_load_logit<DTYPE>(row, id);
@@ -231,28 +268,41 @@ __global__ void __launch_bounds__(THREADS, 4) od_score_kernel(const ScoreArgs A)
     const int nvec = (V - 1) / VEC<DTYPE> + 1;
     const int lo = (int)((int64_t)nvec * part / split), hi = (int)((int64_t)nvec * (part + 1) / split);
     const uint4 none = make_uint4(NONE<DTYPE>, NONE<DTYPE>, NONE<DTYPE>, NONE<DTYPE>);
+    // turns of the loop to a slot: 2^per
+    const int turns = (hi - lo + U * THREADS - 1) / (U * THREADS);
+    int per = 0;
+    while (turns > SLOTS << per) ++per;
     Sums t = {-FLT_MAX, 0.f, 0.f};
+    uint4 x[U];
     {
-        uint4 x[U], y[U];
-        int i = lo + tid;
+        uint4 y[U];
+        int i = lo + tid, turn = 0;
+        float most = -INFINITY;
+        auto take = [&]() {
+            const float m = absorb<DTYPE>(t, x, scale);
+            if (TOP) {
+                most = fmaxf(most, m);
+                if ((++turn & (1 << per) - 1) == 0 || turn == turns) { maxima[(turn - 1) >> per][tid] = most; most = -INFINITY; }
+            }
+        };
 #pragma unroll
         for (int u = 0; u < U; ++u) x[u] = i + u * THREADS < hi ? load_vec<DTYPE>(row, i + u * THREADS, V) : none;
-        for (i += U * THREADS; i < hi; i += U * THREADS) {
+        // (a thread takes part in the last turn even where its loads are behind the end)
+        for (int k = 1; k < turns; ++k) {
+            i += U * THREADS;
 #pragma unroll
             for (int u = 0; u < U; ++u) y[u] = i + u * THREADS < hi ? load_vec<DTYPE>(row, i + u * THREADS, V) : none;
-            absorb<DTYPE>(t, x, scale);
+            take();
 #pragma unroll
             for (int u = 0; u < U; ++u) x[u] = y[u];
         }
-        absorb<DTYPE>(t, x, scale);
+        if (turns > 0) take();
     }
     if (TOP) {
         float g = t.c;
 #pragma unroll
         for (int o = 1; o < 8; o <<= 1) g = fmaxf(g, __shfl_xor_sync(0xFFFFFFFFu, g, o));
         if ((lane & 7) == 0) group_max[tid >> 3] = g;
-        if (tid == 0) n_cand = 0;
-        if (tid < n) { list_v[tid] = -INFINITY; list_i[tid] = -1; }
     }
     const Sums w = warp_total(t, scale);
     if (lane == 0) warp_sums[warp] = w;
@@ -262,19 +312,63 @@ __global__ void __launch_bounds__(THREADS, 4) od_score_kernel(const ScoreArgs A)
         const float g = group_max[lane];
         int rank = 0;
 #pragma unroll
-        for (int k = 0; k < GROUPS; ++k) rank += before(group_max[k], k, g, lane);
+        for (int k = 0; k < GROUPS; ++k) rank += group_max[k] > g || (group_max[k] == g && k < lane);
         const float bound = __shfl_sync(0xFFFFFFFFu, g, __ffs(__ballot_sync(0xFFFFFFFFu, rank == n - 1)) - 1);
-        for (unsigned left = __ballot_sync(0xFFFFFFFFu, t.c >= bound); left; left &= left - 1) {
-            // the elements of one thread, a vector to each lane
-            for (int i = lo + warp * 32 + __ffs(left) - 1 + lane * THREADS; i < hi; i += 32 * THREADS) {
-                const uint4 x = load_vec<DTYPE>(row, i, V);
+        // by whole warps: a place for what reaches the bound (which is at least -FLT_MAX) in N vectors of each lane
+        auto offer = [&](const uint4 *x, const int *at, int N) {
+            int here = 0;
 #pragma unroll
-                for (int k = 0; k < VEC<DTYPE>; ++k) {
-                    const float v = element<DTYPE>(x, k);
-                    if (v >= bound) {                      // (the bound is at least -FLT_MAX)
-                        const int at = atomicAdd(&n_cand, 1);
-                        if (at < CAP) { cand_v[at] = v; cand_i[at] = i * VEC<DTYPE> + k; }
+            for (int u = 0; u < N; ++u)
+#pragma unroll
+                for (int k = 0; k < VEC<DTYPE>; ++k) here += element<DTYPE>(x[u], k) >= bound;
+            int before = here;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(0xFFFFFFFFu, before, o);
+                if (lane >= o) before += v;
+            }
+            const int sum = __shfl_sync(0xFFFFFFFFu, before, 31);
+            if (sum == 0) return;
+            int place = 0;
+            if (lane == 0) place = atomicAdd(&n_cand, sum);
+            place = __shfl_sync(0xFFFFFFFFu, place, 0) + before - here;
+            if (here)
+#pragma unroll
+                for (int u = 0; u < N; ++u)
+#pragma unroll
+                    for (int k = 0; k < VEC<DTYPE>; ++k) {
+                        const float v = element<DTYPE>(x[u], k);
+                        if (v < bound || v != v) continue;
+                        if (place < CAP) cand[place] = key_of(v, at[u] * VEC<DTYPE> + k);
+                        ++place;
                     }
+        };
+        if (turns <= 1) {                                  // all that a thread has read is still in its registers
+            int at[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) at[u] = lo + tid + u * THREADS;
+            offer(x, at, U);
+        } else {
+            if (t.c >= bound)
+                for (int k = 0; k <= (turns - 1) >> per; ++k)
+                    if (maxima[k][tid] >= bound) {
+                        const int at = atomicAdd(&n_again, 1);
+                        if (at < AGAIN) again[at] = (unsigned short)(k << 8 | tid);
+                    }
+            __syncthreads();
+            if (n_again > AGAIN) {
+                if (tid == 0) n_cand = CAP + 1;
+            } else {
+                const int each = U << per;                 // vectors of a slot
+                for (int j0 = 0; j0 < n_again * each; j0 += THREADS) {
+                    const int j = j0 + tid;
+                    int i = hi;
+                    if (j < n_again * each) {
+                        const int what = again[j / each];
+                        i = lo + (what & 255) + ((what >> 8) * each + j % each) * THREADS;
+                    }
+                    const uint4 v = i < hi ? load_vec<DTYPE>(row, i, V) : none;
+                    offer(&v, &i, 1);
                 }
             }
         }
@@ -284,45 +378,37 @@ __global__ void __launch_bounds__(THREADS, 4) od_score_kernel(const ScoreArgs A)
             // many equal logits, or many of the largest in one thread: each warp lists the best of its elements
             // instead, in the order of their ids, so that of equal ones the first n are all that goes in
             __syncthreads();
-            float lv = -INFINITY;
-            int li = 0x7FFFFFFF;
+            Key l = 0;
             for (int i0 = lo + warp * 32; i0 < hi; i0 += THREADS) {
                 const int i = i0 + lane;
-                const uint4 x = i < hi ? load_vec<DTYPE>(row, i, V) : none;
-                const float last_v = __shfl_sync(0xFFFFFFFFu, lv, n - 1);
-                const int last_i = __shfl_sync(0xFFFFFFFFu, li, n - 1);
+                const uint4 v = i < hi ? load_vec<DTYPE>(row, i, V) : none;
+                const Key last = __shfl_sync(0xFFFFFFFFu, l, n - 1);
 #pragma unroll
                 for (int k = 0; k < VEC<DTYPE>; ++k) {
-                    const float v = element<DTYPE>(x, k);
-                    unsigned in = __ballot_sync(0xFFFFFFFFu, v >= bound && before(v, i * VEC<DTYPE> + k, last_v, last_i));
-                    for (; in; in &= in - 1) {
-                        const int from = __ffs(in) - 1;
-                        list_insert(lv, li, __shfl_sync(0xFFFFFFFFu, v, from), (i0 + from) * VEC<DTYPE> + k, lane);
-                    }
+                    const Key mine = key_of(element<DTYPE>(v, k), i * VEC<DTYPE> + k);
+                    unsigned in = __ballot_sync(0xFFFFFFFFu, element<DTYPE>(v, k) >= bound && mine > last);
+                    for (; in; in &= in - 1) list_insert(l, __shfl_sync(0xFFFFFFFFu, mine, __ffs(in) - 1), lane);
                 }
             }
-            if (lane < n) { cand_v[warp * n + lane] = lv; cand_i[warp * n + lane] = li; }
+            if (lane < n) cand[warp * n + lane] = l;
             __syncthreads();
             count = WARPS * n;
         }
-        for (int j = tid; j < count; j += THREADS) {       // rank by counting
-            const float v = cand_v[j];
-            const int i = cand_i[j];
-            int rank = 0;
-            for (int k = 0; k < count; ++k) rank += before(cand_v[k], cand_i[k], v, i);
-            if (v > -INFINITY && rank < n) { list_v[rank] = v; list_i[rank] = i; }
+        if (split > 1) od_cluster_wait();
+        for (int j = tid; j < count; j += THREADS) {       // rank by counting (behind the last is none)
+            const Key k = cand[j];
+            const int rank = keys_in_front(cand, (count + 3) & ~3, k);
+            if (k && rank < n) store_cluster(best + part * n + rank, 0, k);
         }
-        __syncthreads();
+        if (tid < n && tid >= count) store_cluster(best + part * n + tid, 0, (Key)0);
+        if (tid == 0) store_cluster(filled_of + part, 0, min(count, n));
+    } else if (split > 1) {
+        od_cluster_wait();
     }
     // the parts of the row to its cluster's first block
     Sums all = {-FLT_MAX, 0.f, 0.f};
     if (lane < WARPS) all = warp_sums[lane];
     all = warp_total(all, scale);
-    od_cluster_wait();
-    if (TOP && tid < n) {
-        store_cluster(best_v + part * n + tid, 0, list_v[tid]);
-        store_cluster(best_i + part * n + tid, 0, list_i[tid]);
-    }
     if (tid < 3) store_cluster((float *)(block_sums + part) + tid, 0, tid == 0 ? all.c : tid == 1 ? all.s : all.a);
     od_cluster_arrive();
     if (part != 0) return;                                 // (nobody writes into this block)
@@ -343,24 +429,31 @@ __global__ void __launch_bounds__(THREADS, 4) od_score_kernel(const ScoreArgs A)
         if (A.flags) A.flags[r] = (finite ? 0u : OD_LF_NONFINITE) | (empty ? OD_LF_NO_MASS : 0u) | bad_id;
     }
     if (TOP) {
-        const int count = (int)split * n;
         if (!finite) {
             if (tid < n) { A.top_ids[r * n + tid] = -1; A.top_logprobs[r * n + tid] = nan; }
             return;
         }
-        int filled = 0;                                    // alternatives that there are
-        for (int k = 0; k < count; ++k) filled += best_i[k] >= 0;
-        for (int j = tid; j < count; j += THREADS) {
-            const float v = best_v[j];
-            const int i = best_i[j];
-            if (i < 0) continue;
+        // the blocks' lists are in order: a key's place is the sum of its places in all of them
+        if (tid < (int)split * n) {                        // (at most THREADS)
+            const Key k = best[tid];
+            int at[MAX_SPLIT] = {};
+#pragma unroll
+            for (int o = OD_MAX_TOP; o > 0; o >>= 1) {
+                if (o > n) continue;
+#pragma unroll
+                for (int p = 0; p < MAX_SPLIT; ++p)
+                    if (p < (int)split && at[p] + o <= n && best[p * n + at[p] + o - 1] > k) at[p] += o;
+            }
             int rank = 0;
-            for (int k = 0; k < count; ++k) rank += best_i[k] >= 0 && before(best_v[k], best_i[k], v, i);
-            if (rank < n) {
-                A.top_ids[r * n + rank] = i;
-                A.top_logprobs[r * n + rank] = (v - all.c) / T - ln_s;
+#pragma unroll
+            for (int p = 0; p < MAX_SPLIT; ++p) rank += at[p];
+            if (k && rank < n) {
+                A.top_ids[r * n + rank] = id_of(k);
+                A.top_logprobs[r * n + rank] = (logit_of(k) - all.c) / T - ln_s;
             }
         }
+        int filled = 0;
+        for (int p = 0; p < (int)split; ++p) filled += filled_of[p];
         if (tid < n && tid >= filled) { A.top_ids[r * n + tid] = -1; A.top_logprobs[r * n + tid] = -INFINITY; }
     }
 }
@@ -521,9 +614,11 @@ cudaError_t od_launch_score(const od_ctx *c, int32_t B, int32_t R, int32_t V, co
                             uint32_t *flags, cudaStream_t s)
 {
     const int64_t esz = dtype == OD_BF16 ? 2 : 4, rows = (int64_t)B * R;
-    // Blocks of a row: as many as give every multiprocessor two, while a block's slice stays 8 KB or more.
+    // Blocks of a row: one for many rows, up to 8 where there are few, at most three for every multiprocessor and none of a
+    // slice below 16 KB. (us with 20 alternatives, 1 / 2 / 4 / 8 blocks a row: one row of 152064 bf16 logits 21 / 14 / 11 / 10,
+    // 96 rows of 128256 18.7 / 15.7 / 16.4 / 21, 448 rows 39 / 40 / 48 / 70, 4608 rows of 152064 290 / 345 / 461 / 738.)
     int32_t split = 1;
-    while (split < MAX_SPLIT && rows * split < 2 * c->sm_count && (int64_t)V * esz / split >= 16384) split *= 2;
+    while (split < MAX_SPLIT && rows * split * 2 <= 3 * c->sm_count && (int64_t)V * esz / (split * 2) >= 16384 - 256) split *= 2;
     const ScoreArgs a = {(const char *)logits, row_stride * esz, seq_stride * esz, R, V, n_top, split, ids, n_rows, temperature,
                          logprob, entropy, row_max, row_sum, top_logprobs, top_ids, flags};
     const unsigned blocks = (unsigned)(rows * split);
