@@ -689,7 +689,7 @@ int32_t od_token_logprobs_grad(od_ctx *c, int32_t B, int32_t R, int32_t vocab, c
     if (n_top < 0 || n_top > OD_MAX_TOP || !row_max || !row_sum) return OD_ERR_INVALID_ARG;
     if ((g_top && (n_top == 0 || !top_ids)) || (g_entropy && !entropy)) return OD_ERR_INVALID_ARG;
     if (grad == logits && (grad_row_stride != row_stride || grad_seq_stride != seq_stride)) return OD_ERR_INVALID_ARG;
-    if (od_score_grad_blocks((int64_t)B * R, vocab, logit_dtype) > INT32_MAX) return OD_ERR_UNSUPPORTED;
+    if (od_score_grad_blocks((int64_t)B * R, vocab, logit_dtype, c->sm_count) > INT32_MAX) return OD_ERR_UNSUPPORTED;
     DeviceGuard g(c->device);
     if (!g.ok) return OD_ERR_CUDA;
     OD_CUDA(od_launch_score_grad(c, B, R, vocab, logits, logit_dtype, row_stride, seq_stride, ids, n_rows, temperature, row_max,

@@ -314,7 +314,7 @@ cudaError_t od_launch_score(const od_ctx *c, int32_t B, int32_t R, int32_t V, co
                             int64_t seq_stride, const int32_t *ids, const int32_t *n_rows, const float *temperature, int32_t n_top,
                             float *logprob, float *entropy, float *row_max, float *row_sum, int32_t *top_ids, float *top_logprobs,
                             uint32_t *flags, cudaStream_t s);
-int64_t od_score_grad_blocks(int64_t rows, int32_t V, int32_t dtype);   // of the launch below
+int64_t od_score_grad_blocks(int64_t rows, int32_t V, int32_t dtype, int32_t sms);   // of the launch below
 cudaError_t od_launch_score_grad(const od_ctx *c, int32_t B, int32_t R, int32_t V, const void *logits, int32_t dtype, int64_t row_stride,
                                  int64_t seq_stride, const int32_t *ids, const int32_t *n_rows, const float *temperature,
                                  const float *row_max, const float *row_sum, const float *entropy, int32_t n_top,

@@ -29,6 +29,7 @@ constexpr int GROUPS = THREADS / 8;                        // of eight threads
 constexpr int U = 4;                                       // 16-byte loads of a thread in flight
 constexpr int MAX_SPLIT = 8;                               // blocks of a row (a portable cluster)
 constexpr int CAP = 512;                                   // candidates that are ranked by counting
+constexpr int GRAD_TURNS = 8;
 constexpr int SLOTS = 32;                                  // maxima that a thread leaves
 constexpr int AGAIN = 256;                                 // of them that are looked at again
 constexpr float LEAST = -150.f;                            // exp2 of it is zero
@@ -276,27 +277,36 @@ __global__ void __launch_bounds__(THREADS, 4) od_score_kernel(const ScoreArgs A)
     uint4 x[U];
     {
         uint4 y[U];
-        int i = lo + tid, turn = 0;
-        float most = -INFINITY;
-        auto take = [&]() {
-            const float m = absorb<DTYPE>(t, x, scale);
-            if (TOP) {
-                most = fmaxf(most, m);
-                if ((++turn & (1 << per) - 1) == 0 || turn == turns) { maxima[(turn - 1) >> per][tid] = most; most = -INFINITY; }
+        // turns whose loads are all whole vectors of this block's slice
+        const int whole = max(0, min(hi, V / VEC<DTYPE>) - lo) / (U * THREADS);
+        const char *next = row + (size_t)(lo + tid) * 16;
+        auto load = [&](uint4 (&v)[U], int turn) {
+            if (turn < whole) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) v[u] = ld_stream(next + u * THREADS * 16);
+                next += U * THREADS * 16;
+            } else {
+                const int i = lo + tid + turn * (U * THREADS);
+#pragma unroll
+                for (int u = 0; u < U; ++u) v[u] = i + u * THREADS < hi ? load_vec<DTYPE>(row, i + u * THREADS, V) : none;
             }
         };
-#pragma unroll
-        for (int u = 0; u < U; ++u) x[u] = i + u * THREADS < hi ? load_vec<DTYPE>(row, i + u * THREADS, V) : none;
-        // (a thread takes part in the last turn even where its loads are behind the end)
-        for (int k = 1; k < turns; ++k) {
-            i += U * THREADS;
-#pragma unroll
-            for (int u = 0; u < U; ++u) y[u] = i + u * THREADS < hi ? load_vec<DTYPE>(row, i + u * THREADS, V) : none;
-            take();
-#pragma unroll
-            for (int u = 0; u < U; ++u) x[u] = y[u];
+        auto take = [&](const uint4 (&v)[U], int turn) {
+            float m = absorb<DTYPE>(t, v, scale);
+            if (TOP) {
+                float &most = maxima[turn >> per][tid];
+                if (turn & (1 << per) - 1) m = fmaxf(m, most);
+                most = m;
+            }
+        };
+        load(x, 0);
+        for (int k = 0; k < turns; k += 2) {
+            if (k + 1 < turns) load(y, k + 1);
+            take(x, k);
+            if (k + 1 == turns) break;
+            if (k + 2 < turns) load(x, k + 2);
+            take(y, k + 1);
         }
-        if (turns > 0) take();
     }
     if (TOP) {
         float g = t.c;
@@ -465,12 +475,11 @@ struct ScoreGradArgs {
     int64_t row_bytes, seq_bytes;
     char *grad;
     int64_t grad_row_bytes, grad_seq_bytes;
-    int32_t R, V, n_top, chunks;                           // blocks of a row
+    int32_t R, V, n_top, chunks, turns;                    // blocks of a row, loads of U vectors of a thread
     const int32_t *ids, *n_rows, *top_ids;
     const float *temperature, *row_max, *row_sum, *entropy, *g_logprob, *g_entropy, *g_top;
 };
 
-constexpr int CHUNK = U * THREADS;                         // vectors of a block
 
 __device__ __forceinline__ uint32_t bf16x2(float lo, float hi)
 {
@@ -485,15 +494,20 @@ __device__ __forceinline__ void store_element(char *row, int j, float v)
     else ((unsigned short *)row)[j] = (unsigned short)bf16x2(v, 0.f);
 }
 template <int DTYPE>
+__device__ __forceinline__ void store_whole(char *at, const float (&v)[VEC<DTYPE>])
+{
+    uint4 o;
+    if constexpr (DTYPE == OD_F32)
+        o = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    else
+        o = make_uint4(bf16x2(v[0], v[1]), bf16x2(v[2], v[3]), bf16x2(v[4], v[5]), bf16x2(v[6], v[7]));
+    *(uint4 *)at = o;
+}
+template <int DTYPE>
 __device__ __forceinline__ void store_vec(char *row, int i, int V, const float (&v)[VEC<DTYPE>])
 {
     if (i < V / VEC<DTYPE>) {
-        uint4 o;
-        if constexpr (DTYPE == OD_F32)
-            o = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-        else
-            o = make_uint4(bf16x2(v[0], v[1]), bf16x2(v[2], v[3]), bf16x2(v[4], v[5]), bf16x2(v[6], v[7]));
-        *(uint4 *)(row + (size_t)i * 16) = o;
+        store_whole<DTYPE>(row + (size_t)i * 16, v);
         return;
     }
 #pragma unroll
@@ -503,7 +517,7 @@ __device__ __forceinline__ void store_vec(char *row, int i, int V, const float (
 
 // grad may be the logits themselves: an element is written by the thread that has read it, the given ones behind a
 // barrier from logits that were read in front of it.
-template <int DTYPE>
+template <int DTYPE, bool ENTROPY>
 __global__ void __launch_bounds__(THREADS) od_score_grad_kernel(const ScoreGradArgs A)
 {
     constexpr int GIVEN = OD_MAX_TOP + 1;
@@ -518,7 +532,7 @@ __global__ void __launch_bounds__(THREADS) od_score_grad_kernel(const ScoreGradA
     const int32_t b = (int32_t)(r / A.R), rr = (int32_t)(r % A.R);
     const char *row = A.logits + b * A.seq_bytes + rr * A.row_bytes;
     char *out = A.grad + b * A.grad_seq_bytes + rr * A.grad_row_bytes;
-    const int nvec = (V - 1) / VEC<DTYPE> + 1, lo = chunk * CHUNK, hi = min(nvec, lo + CHUNK);
+    const int nvec = (V - 1) / VEC<DTYPE> + 1, per_block = A.turns * (U * THREADS), lo = chunk * per_block, hi = min(nvec, lo + per_block);
     const bool counts = !A.n_rows || rr < A.n_rows[b];
     const float T = A.temperature ? A.temperature[b] : 1.f;
     const float S = counts ? A.row_sum[r] : 0.f;
@@ -527,10 +541,20 @@ __global__ void __launch_bounds__(THREADS) od_score_grad_kernel(const ScoreGradA
         for (int i = lo + tid; i < hi; i += THREADS) store_vec<DTYPE>(out, i, V, zero);
         return;
     }
-    uint4 x[U];
+    const int whole = max(0, min(hi, V / VEC<DTYPE>) - lo) / (U * THREADS), turns = (hi - lo + U * THREADS - 1) / (U * THREADS);
+    auto load = [&](uint4 (&v)[U], int turn) {
+        const int i = lo + turn * (U * THREADS) + tid;
+        if (turn < whole) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-        if (lo + u * THREADS + tid < hi) x[u] = load_vec<DTYPE, false>(row, lo + u * THREADS + tid, V);
+            for (int u = 0; u < U; ++u) v[u] = __ldcs((const uint4 *)(row + (size_t)i * 16) + u * THREADS);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i + u * THREADS < hi) v[u] = load_vec<DTYPE, false>(row, i + u * THREADS, V);
+        }
+    };
+    uint4 x[U], y[U];
+    load(x, 0);
 
     // every warp sums the weights itself, in the same order
     const float M = A.row_max[r], ln_s = logf(S), scale = LOG2E / T;
@@ -549,8 +573,8 @@ __global__ void __launch_bounds__(THREADS) od_score_grad_kernel(const ScoreGradA
     if (tid < 32) { given_id[lane] = top; given_g[lane] = g; }
     if (tid == 0) { given_id[OD_MAX_TOP] = given ? id : -1; given_g[OD_MAX_TOP] = g_id; }
     __syncthreads();
-    const float g_h = A.g_entropy ? A.g_entropy[r] : 0.f, per = -1.f / (S * T);
-    const float c0 = per * (G + (A.g_entropy ? g_h * (A.entropy[r] - ln_s) : 0.f)), c1 = per * g_h * LN2;
+    const float g_h = ENTROPY ? A.g_entropy[r] : 0.f, per = -1.f / (S * T);
+    const float c0 = per * (G + (ENTROPY ? g_h * (A.entropy[r] - ln_s) : 0.f)), c1 = per * g_h * LN2;
 
     // the value of a given id in this chunk: it is written by the first entry that names it, with the sum of their weights
     int write = -1;
@@ -565,7 +589,7 @@ __global__ void __launch_bounds__(THREADS) od_score_grad_kernel(const ScoreGradA
             if (first) {
                 const float xj = DTYPE == OD_F32 ? __ldcs((const float *)row + j) : __uint_as_float((uint32_t)__ldcs((const unsigned short *)row + j) << 16);
                 const float d = (xj - M) * scale;
-                value = od_ex2(d) * (c0 + c1 * fmaxf(d, LEAST)) + sum / T;
+                value = od_ex2(d) * (ENTROPY ? c0 + c1 * fmaxf(d, LEAST) : c0) + sum / T;
                 write = j;
             }
         }
@@ -573,19 +597,30 @@ __global__ void __launch_bounds__(THREADS) od_score_grad_kernel(const ScoreGradA
     // (in front of every store: they may be to the logits that were read above)
     __syncthreads();
     const uint64_t nm2 = f2_pack(-M, -M), scale2 = f2_pack(scale, scale), c02 = f2_pack(c0, c0), c12 = f2_pack(c1, c1);
+    auto put = [&](const uint4 (&v)[U], int turn) {
+        const int i = lo + turn * (U * THREADS) + tid;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int i = lo + u * THREADS + tid;
-        if (i >= hi) break;
-        float v[VEC<DTYPE>];
+        for (int u = 0; u < U; ++u) {
+            if (turn >= whole && i + u * THREADS >= hi) break;
+            float w[VEC<DTYPE>];
 #pragma unroll
-        for (int k = 0; k < VEC<DTYPE>; k += 2) {
-            float d0, d1;
-            f2_unpack(f2_mul(f2_add(f2_pack(element<DTYPE>(x[u], k), element<DTYPE>(x[u], k + 1)), nm2), scale2), d0, d1);
-            const uint64_t e2 = f2_pack(od_ex2(d0), od_ex2(d1));
-            f2_unpack(f2_mul(e2, f2_fma(f2_pack(fmaxf(d0, LEAST), fmaxf(d1, LEAST)), c12, c02)), v[k], v[k + 1]);
+            for (int k = 0; k < VEC<DTYPE>; k += 2) {
+                float d0, d1;
+                f2_unpack(f2_mul(f2_add(f2_pack(element<DTYPE>(v[u], k), element<DTYPE>(v[u], k + 1)), nm2), scale2), d0, d1);
+                const uint64_t e2 = f2_pack(od_ex2(d0), od_ex2(d1));
+                f2_unpack(f2_mul(e2, ENTROPY ? f2_fma(f2_pack(fmaxf(d0, LEAST), fmaxf(d1, LEAST)), c12, c02) : c02), w[k], w[k + 1]);
+            }
+            if (turn < whole) store_whole<DTYPE>(out + ((size_t)i + u * THREADS) * 16, w);
+            else store_vec<DTYPE>(out, i + u * THREADS, V, w);
         }
-        store_vec<DTYPE>(out, i, V, v);
+    };
+    // (in place too: a thread has read what it writes, and what it reads ahead is its own)
+    for (int k = 0; k < turns; k += 2) {
+        if (k + 1 < turns) load(y, k + 1);
+        put(x, k);
+        if (k + 1 == turns) break;
+        if (k + 2 < turns) load(x, k + 2);
+        put(y, k + 1);
     }
     __syncthreads();
     if (write >= 0) store_element<DTYPE>(out, write, value);
@@ -614,11 +649,13 @@ cudaError_t od_launch_score(const od_ctx *c, int32_t B, int32_t R, int32_t V, co
                             uint32_t *flags, cudaStream_t s)
 {
     const int64_t esz = dtype == OD_BF16 ? 2 : 4, rows = (int64_t)B * R;
-    // Blocks of a row: one for many rows, up to 8 where there are few, at most three for every multiprocessor and none of a
-    // slice below 16 KB. (us with 20 alternatives, 1 / 2 / 4 / 8 blocks a row: one row of 152064 bf16 logits 21 / 14 / 11 / 10,
-    // 96 rows of 128256 18.7 / 15.7 / 16.4 / 21, 448 rows 39 / 40 / 48 / 70, 4608 rows of 152064 290 / 345 / 461 / 738.)
+    // Blocks of a row: one for many rows, up to 8 where there are few (of ragged ones half count, about): at most seven for two
+    // multiprocessors, and none of a slice below 16 KB. (us with 20 alternatives, 1 / 2 / 4 / 8 blocks a row: one row of
+    // 152064 bf16 logits 21 / 14 / 11 / 10, 96 rows of 128256 19 / 16 / 16 / 21, 448 rows 39 / 40 / 48 / 70, 4608 rows of
+    // 152064 290 / 345 / 461 / 738.)
+    const int64_t count = n_rows ? (rows + 1) / 2 : rows;
     int32_t split = 1;
-    while (split < MAX_SPLIT && rows * split * 2 <= 3 * c->sm_count && (int64_t)V * esz / (split * 2) >= 16384 - 256) split *= 2;
+    while (split < MAX_SPLIT && count * split * 4 <= 7 * c->sm_count && (int64_t)V * esz / (split * 2) >= 16384 - 256) split *= 2;
     const ScoreArgs a = {(const char *)logits, row_stride * esz, seq_stride * esz, R, V, n_top, split, ids, n_rows, temperature,
                          logprob, entropy, row_max, row_sum, top_logprobs, top_ids, flags};
     const unsigned blocks = (unsigned)(rows * split);
@@ -628,10 +665,19 @@ cudaError_t od_launch_score(const od_ctx *c, int32_t B, int32_t R, int32_t V, co
     return n_top ? launch(od_score_kernel<OD_F32, true>, blocks, split, pdl, a, s) : launch(od_score_kernel<OD_F32, false>, blocks, split, pdl, a, s);
 }
 
-int64_t od_score_grad_blocks(int64_t rows, int32_t V, int32_t dtype)
+// Loads of a thread: up to 8, as long as there are eight blocks for every multiprocessor
+static int32_t grad_turns(int64_t rows, int32_t nvec, int32_t sms)
+{
+    int32_t turns = 1;
+    while (turns < GRAD_TURNS && rows * nvec / (U * THREADS * 2 * turns) >= 8 * (int64_t)sms) turns *= 2;
+    return turns;
+}
+
+int64_t od_score_grad_blocks(int64_t rows, int32_t V, int32_t dtype, int32_t sms)
 {
     const int32_t nvec = dtype == OD_BF16 ? (V - 1) / VEC<OD_BF16> + 1 : (V - 1) / VEC<OD_F32> + 1;
-    return rows * ((nvec + CHUNK - 1) / CHUNK);
+    const int32_t chunk = U * THREADS * grad_turns(rows, nvec, sms);
+    return rows * ((nvec + chunk - 1) / chunk);
 }
 
 cudaError_t od_launch_score_grad(const od_ctx *c, int32_t B, int32_t R, int32_t V, const void *logits, int32_t dtype, int64_t row_stride,
@@ -640,10 +686,13 @@ cudaError_t od_launch_score_grad(const od_ctx *c, int32_t B, int32_t R, int32_t 
                                  const int32_t *top_ids, const float *g_logprob, const float *g_entropy, const float *g_top, void *grad,
                                  int64_t grad_row_stride, int64_t grad_seq_stride, cudaStream_t s)
 {
-    const int64_t esz = dtype == OD_BF16 ? 2 : 4, blocks = od_score_grad_blocks((int64_t)B * R, V, dtype);
+    const int64_t esz = dtype == OD_BF16 ? 2 : 4, rows = (int64_t)B * R, blocks = od_score_grad_blocks(rows, V, dtype, c->sm_count);
+    const int32_t nvec = (int32_t)(((int64_t)V * esz + 15) / 16);
     const ScoreGradArgs a = {(const char *)logits, row_stride * esz, seq_stride * esz, (char *)grad, grad_row_stride * esz,
-                             grad_seq_stride * esz, R, V, n_top, (int32_t)(blocks / ((int64_t)B * R)), ids, n_rows, top_ids, temperature,
-                             row_max, row_sum, entropy, g_logprob, g_entropy, g_top};
-    return dtype == OD_BF16 ? launch(od_score_grad_kernel<OD_BF16>, (unsigned)blocks, 1, c->opt_pdl != 0, a, s)
-                            : launch(od_score_grad_kernel<OD_F32>, (unsigned)blocks, 1, c->opt_pdl != 0, a, s);
+                             grad_seq_stride * esz, R, V, n_top, (int32_t)(blocks / rows), grad_turns(rows, nvec, c->sm_count), ids,
+                             n_rows, top_ids, temperature, row_max, row_sum, entropy, g_logprob, g_entropy, g_top};
+    const bool pdl = c->opt_pdl != 0;
+    if (dtype == OD_BF16)
+        return g_entropy ? launch(od_score_grad_kernel<OD_BF16, true>, (unsigned)blocks, 1, pdl, a, s) : launch(od_score_grad_kernel<OD_BF16, false>, (unsigned)blocks, 1, pdl, a, s);
+    return g_entropy ? launch(od_score_grad_kernel<OD_F32, true>, (unsigned)blocks, 1, pdl, a, s) : launch(od_score_grad_kernel<OD_F32, false>, (unsigned)blocks, 1, pdl, a, s);
 }
