@@ -63,6 +63,18 @@ __device__ __forceinline__ uint4 lds128(uint32_t at)
     asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
     return v;
 }
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -465,23 +477,37 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
     int fs = slab, slot_f = 0;
     const uint32_t put = ring + (lane >> 2) * 64 + ((t ^ (lane >> 4)) << 4);
     const uint8_t *const from = A.codes + (size_t)col / 2 + t * 16;
+    const uint8_t *code_at = from + (size_t)(slab * G_ROWS + (lane >> 2)) * row_bytes;
+    const size_t code_step = (size_t)slabs * G_ROWS * row_bytes, eight = 8 * row_bytes;
+    constexpr int ITEMS = 8 * NT * PIECES / 32;            // pieces of tokens of a lane: of tokens 32 / PIECES apart
+    const int n_at = lane / PIECES, c_at = lane % PIECES;
+    const uint32_t put_d = ring + G_CODES + n_at * (PIECES * 16) + ((c_at ^ (F32 ? (n_at & 1) << 2 : (n_at >> 1 & 1) << 1)) << 4);
+    const char *d_at = (const char *)A.in + ((int64_t)(n0 + n_at) * A.in_stride + slab * G_ROWS + c_at * (16 / ESZ)) * ESZ;
+    const int64_t d_step = (int64_t)slabs * G_ROWS * ESZ, d_token = 32 / PIECES * A.in_stride * ESZ;
     auto fetch = [&]() {
         if (fs < steps) {
-            const int r = fs * G_ROWS + (lane >> 2);
             const uint32_t to = put + slot_f;
-            if (t < here) {
+            if (t < here) {                                // (rows 8 on: the piece's place has another bit)
+                if (fs * G_ROWS + G_ROWS <= V) {
+                    cp16(to, code_at);
+                    cp16((to + 8 * 64) ^ 32, code_at + eight);
+                    cp16(to + 16 * 64, code_at + 2 * eight);
+                    cp16((to + 24 * 64) ^ 32, code_at + 3 * eight);
+                } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)                // (rows 8 on: the piece's place has another bit)
-                    cp16((to + i * 8 * 64) ^ (i & 1 ? 32 : 0), from + (size_t)min(r + 8 * i, V - 1) * row_bytes);
+                    for (int i = 0; i < 4; ++i)
+                        cp16((to + i * 8 * 64) ^ (i & 1 ? 32 : 0), from + (size_t)min(fs * G_ROWS + (lane >> 2) + 8 * i, V - 1) * row_bytes);
+                }
             }
+            const int bytes = max(0, min(16 / ESZ, V - (fs * G_ROWS + c_at * (16 / ESZ)))) * ESZ;
 #pragma unroll
-            for (int i = 0; i < 8 * NT * PIECES / 32; ++i) {
-                const int n = (i * 32 + lane) / PIECES, c = lane % PIECES, v = fs * G_ROWS + c * (16 / ESZ);
-                const int bytes = n0 + n < A.N ? max(0, min(16 / ESZ, V - v)) * ESZ : 0;
-                const char *at = (const char *)A.in + (bytes ? (int64_t)(n0 + n) * A.in_stride + v : 0) * ESZ;
-                cp16_part(ring + slot_f + G_CODES + n * (PIECES * 16) + ((c ^ (F32 ? (n & 1) << 2 : (n >> 1 & 1) << 1)) << 4), at, bytes);
+            for (int i = 0; i < ITEMS; ++i) {
+                const bool in = bytes > 0 && n0 + n_at + i * (32 / PIECES) < A.N;
+                cp16_part(put_d + slot_f + i * 512, in ? d_at + i * d_token : A.in, in ? bytes : 0);
             }
             fs += slabs;
+            code_at += code_step;
+            d_at += d_step;
         }
         cp_commit();
         slot_f = slot_f + STAGE == G_RING * STAGE ? 0 : slot_f + STAGE;
@@ -501,12 +527,13 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
     constexpr bool PAIRS = GB > 1;
     const uint32_t get = ring + 4 * t * 64 + (PAIRS ? g & 3 : g >> 1) * 4, pick = g & 1 ? HIGH : LOW;
     const uint32_t get_d = ring + G_CODES + g * (PIECES * 16) + (F32 ? (t ^ (g & 1) << 2) << 4 : (g >> 1 & 1) << 5 | t << 3);
-    float acc[8][NT][4] = {}, eights[GROUPS][NT] = {};
+    float acc[8][NT][4] = {};
+    uint64_t eights[GROUPS][NT] = {};                      // pairs of sums
     int slot = 0, flip = 0;
     if (slab < steps) load_scales(slab);
     for (int s = slab; s < steps; s += slabs) {
 #pragma unroll
-        for (int i = 0; i < GROUPS; ++i) scale_of[(flip * G_ROWS + lane) * GROUPS + i] = raw.get(i);
+        for (int i = 0; i < GROUPS; ++i) scale_of[(flip * G_ROWS + lane) * GROUPS + i] = raw.get(i) * UP;
         if (s + slabs < steps) load_scales(s + slabs);
         cp_wait<G_RING - 2>();
         __syncwarp();
@@ -539,28 +566,36 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
 #pragma unroll
         for (int i = 0; i < GROUPS; ++i) {
             if (i * GB >= here) break;
-            float z[2][NT][4], m = 0.f;
+            uint64_t z[2][NT][2];                          // pairs of rows
+            float m = 0.f;
 #pragma unroll
             for (int half = 0; half < 2; ++half)
 #pragma unroll
-                for (int q = 0; q < NT; ++q) {
+                for (int q = 0; q < NT; ++q)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        z[half][q][k] = d[half][q][k] * e[half][k][i] * UP;
-                        m = fmaxf(m, fabsf(z[half][q][k]));
+                    for (int k = 0; k < 2; ++k) {
+                        z[half][q][k] = f2_mul(f2_pack(d[half][q][2 * k], d[half][q][2 * k + 1]), f2_pack(e[half][2 * k][i], e[half][2 * k + 1][i]));
+                        float lo, hi;
+                        f2_unpack(z[half][q][k], lo, hi);
+                        m = max_nan(max_nan(m, fabsf(lo)), fabsf(hi));
                     }
-                }
-            // (NaN is not in the maximum: its pieces are, and the sum is NaN)
-            if (__any_sync(0xFFFFFFFFu, m == INFINITY)) {
+            if (__any_sync(0xFFFFFFFFu, !(m < INFINITY))) {
+                // too large to be scaled, infinite or NaN (or nothing, and the scale too large)
 #pragma unroll
                 for (int half = 0; half < 2; ++half)
 #pragma unroll
                     for (int q = 0; q < NT; ++q)
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            const bool large = fabsf(z[half][q][k]) == INFINITY;
-                            const float big = d[half][q][k] * e[half][k][i] * (1.f / BACK);
-                            if (large) z[half][q][k] = 0.f;
+                            float lo, hi;
+                            f2_unpack(z[half][q][k / 2], lo, hi);
+                            const bool large = !(fabsf(k & 1 ? hi : lo) < INFINITY);
+                            float big = 0.f;
+                            if (large) {
+                                const int v = s * G_ROWS + half * 16 + 4 * t + k;      // (behind the last row the scale is zero)
+                                big = d[half][q][k] * (1.f / BACK) * __uint_as_float((uint32_t)A.scales[(size_t)v * n_groups + col / (32 * GB) + i] << 16);
+                                z[half][q][k / 2] = k & 1 ? f2_pack(lo, 0.f) : f2_pack(0.f, hi);
+                            }
                             for (unsigned lanes = __ballot_sync(0xFFFFFFFFu, large); lanes; lanes &= lanes - 1) {
                                 const int src = __ffs(lanes) - 1, n = src >> 2, r = half * 16 + 4 * (src & 3) + k;
                                 const float f = __shfl_sync(0xFFFFFFFFu, big, src);
@@ -581,12 +616,20 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
 #pragma unroll
             for (int half = 0; half < 2; ++half)
 #pragma unroll
-                for (int q = 0; q < NT; ++q) {
-                    pieces<P>(z[half][q][0], z[half][q][1], b[half][q][0]);
-                    pieces<P>(z[half][q][2], z[half][q][3], b[half][q][1]);
+                for (int q = 0; q < NT; ++q)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) eights[i][q] = fmaf(z[half][q][k], 0x1p-126f * 0.0625f, eights[i][q]);     // 8 times 2^-133
-                }
+                    for (int k = 0; k < 2; ++k) {
+                        eights[i][q] = f2_fma(z[half][q][k], f2_pack(0x1p-126f * 0.0625f, 0x1p-126f * 0.0625f), eights[i][q]);      // 8 times 2^-133
+                        uint64_t rest = z[half][q][k];
+#pragma unroll
+                        for (int p = 0; p < P; ++p) {
+                            float lo, hi;
+                            f2_unpack(rest, lo, hi);
+                            b[half][q][k][p] = halves(__float_as_uint(lo), __float_as_uint(hi), HIGH);
+                            if (p + 1 < P)
+                                rest = f2_add(rest, f2_pack(-__uint_as_float(__float_as_uint(lo) & 0xFFFF0000u), -__uint_as_float(__float_as_uint(hi) & 0xFFFF0000u)));
+                        }
+                    }
             // four codes of a lane in each of four rows: two columns of two sums
             auto product = [&](uint32_t w01, uint32_t w23, int half, int c) {
                 const uint32_t v01 = w01 >> 8, v23 = w23 >> 8;
@@ -627,7 +670,9 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
     for (int i = 0; i < GROUPS; ++i)
 #pragma unroll
         for (int q = 0; q < NT; ++q) {
-            float v = eights[i][q];
+            float v, more;
+            f2_unpack(eights[i][q], v, more);
+            v += more;
             v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
             v += __shfl_xor_sync(0xFFFFFFFFu, v, 2);       // of token g
             const float e[2] = {__shfl_sync(0xFFFFFFFFu, v, 8 * t), __shfl_sync(0xFFFFFFFFu, v, 8 * t + 4)};
@@ -650,17 +695,24 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
     }
 }
 
-// the blocks on the same columns: [tile][split][warp side by side][token][column]
-__global__ void od_q4_join_kernel(const Q4Args A, int tokens)
+// The blocks on the same columns: [tile][split][warp side by side][token][column]. A block of threads has 32 numbers,
+// each by eight threads that have every eighth part, and adds theirs in order.
+constexpr int JOIN = 8;
+__global__ void __launch_bounds__(32 * JOIN) od_q4_join_kernel(const Q4Args A, int tokens)
 {
+    __shared__ float sums[JOIN][32];
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int i = blockIdx.x * blockDim.x + threadIdx.x, n = i / A.H, h = i % A.H;
-    if (n >= tokens || A.first_token + n >= A.N) return;
+    const int h = blockIdx.x * 32 + threadIdx.x, n = blockIdx.y;               // (H is a multiple of 32)
     const int size = A.col_warps * tokens * COLS, tile = h / (A.col_warps * COLS);
     const float *p = A.parts + (size_t)tile * A.split * size + (h / COLS % A.col_warps * tokens + n) * COLS + h % COLS;
     float v = 0.f;
 #pragma unroll 8
-    for (int k = 0; k < A.split; ++k) v += p[(size_t)k * size];
+    for (int k = threadIdx.y; k < A.split; k += JOIN) v += p[(size_t)k * size];
+    sums[threadIdx.y][threadIdx.x] = v;
+    __syncthreads();
+    if (threadIdx.y > 0) return;
+#pragma unroll
+    for (int k = 1; k < JOIN; ++k) v += sums[k][threadIdx.x];
     store(A, A.first_token + n, h, v);
 }
 
@@ -702,10 +754,10 @@ Variant variant(bool backward, int32_t G, bool f32, int N, int32_t H)
 }
 
 template <typename K, typename... A>
-cudaError_t launch(K kernel, dim3 grid, int threads, int smem, bool pdl, cudaStream_t s, A... args)
+cudaError_t launch(K kernel, dim3 grid, dim3 threads, int smem, bool pdl, cudaStream_t s, A... args)
 {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid; cfg.blockDim = dim3(threads);
+    cfg.gridDim = grid; cfg.blockDim = threads;
     cfg.dynamicSmemBytes = smem; cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -765,7 +817,7 @@ cudaError_t od_launch_q4(const od_ctx *c, bool backward, int32_t N, int32_t V, i
         args.first_token = n;
         cudaError_t e = launch(v.kernel, dim3((unsigned)blocks), THREADS, v.smem, pdl, s, args);
         if (e == cudaSuccess && args.split > 1)
-            e = launch(od_q4_join_kernel, dim3((unsigned)(((int64_t)v.tokens * H + 255) / 256)), 256, 0, pdl, s, args, v.tokens);
+            e = launch(od_q4_join_kernel, dim3((unsigned)(H / 32), (unsigned)(N - n < v.tokens ? N - n : v.tokens)), dim3(32, JOIN), 0, pdl, s, args, v.tokens);
         if (e != cudaSuccess) return e;
         n += v.tokens;
     }
