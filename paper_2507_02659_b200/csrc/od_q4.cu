@@ -28,7 +28,6 @@ constexpr int COLS = 128;                                  // backward: of a war
 constexpr int G_RING = 3;                                  // backward: stages of a warp
 constexpr int WIDE = 8;                                    // forward: blocks of 32 columns to a stage
 constexpr int WIDE_STAGE = ROWS * WIDE * 16;
-constexpr int WIDE_RING = 3;
 
 struct Q4Args {
     const void *in;                                        // x or dy
@@ -225,7 +224,7 @@ __device__ __noinline__ float one_logit(const Q4Args &A, int n, int v, int G)
     return total;
 }
 
-template <int P, int NT, int GB, bool XS>
+template <int P, int NT, int GB, bool XS, int RING>
 __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
 {
     extern __shared__ __align__(128) unsigned char smem[];
@@ -242,7 +241,7 @@ __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
     const int ks = A.k_split, sub = warp % ks, groups = F_WARPS / ks;
     const int first = stages * sub / ks, last = stages * (sub + 1) / ks;
     const int units = (V + ROWS - 1) / ROWS, step = gridDim.x * groups, begin = blockIdx.x + warp / ks * gridDim.x;
-    unsigned char *const mine = smem + warp * (WIDE_RING * WIDE_STAGE);
+    unsigned char *const mine = smem + warp * (RING * WIDE_STAGE);
     const size_t row_bytes = (size_t)H / 2;
 
     // fetching: this lane copies pieces lane % 4 and 4 + lane % 4 of rows lane / 4 and 8 + lane / 4
@@ -263,10 +262,10 @@ __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
             if (++fs == last) { fs = first; fu += step; }
         }
         cp_commit();
-        slot_f = slot_f + WIDE_STAGE == WIDE_RING * WIDE_STAGE ? 0 : slot_f + WIDE_STAGE;
+        slot_f = slot_f + WIDE_STAGE == RING * WIDE_STAGE ? 0 : slot_f + WIDE_STAGE;
     };
 #pragma unroll
-    for (int i = 0; i < WIDE_RING - 1; ++i) fetch();
+    for (int i = 0; i < RING - 1; ++i) fetch();
 
     // the largest magnitude of each token, by two warps
     for (int i = warp; i < 16 * NT; i += F_WARPS) {
@@ -287,7 +286,7 @@ __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
     auto largest = [&](int n) { return max(largest_of[n][0], largest_of[n][1]); };
 
     // [group][8 tokens to a part]: what the group's sums begin at; [block of 32 columns][part][piece][lane]: the fragments
-    float *const starts = (float *)(smem + F_WARPS * WIDE_RING * WIDE_STAGE);
+    float *const starts = (float *)(smem + F_WARPS * RING * WIDE_STAGE);
     unsigned char *const inputs = (unsigned char *)(starts + n_groups * 8 * NT);
     for (int i = warp; i < n_groups * NT; i += F_WARPS) {
         const int q = i % NT, n = n0 + q * 8 + g;
@@ -348,7 +347,7 @@ __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
             const Scales<GB> s0[2] = {next0[0], next0[1]}, s1[2] = {next1[0], next1[1]};
             if (s + 1 < last) load_scales(s + 1);
             else if (u + step < units) { aim_scales(u + step); load_scales(first); }
-            cp_wait<WIDE_RING - 2>();
+            cp_wait<RING - 2>();
             __syncwarp();
             fetch();
             float sum[NT][4];
@@ -400,7 +399,7 @@ __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
             }
             xs += WIDE * NT * P * 512;
             begin_at += WIDE / GB * NT * 4;
-            slot = slot + WIDE_STAGE == WIDE_RING * WIDE_STAGE ? 0 : slot + WIDE_STAGE;
+            slot = slot + WIDE_STAGE == RING * WIDE_STAGE ? 0 : slot + WIDE_STAGE;
         }
         if (ks > 1) {
             if (sub > 0) {
@@ -716,21 +715,24 @@ __global__ void __launch_bounds__(32 * JOIN) od_q4_join_kernel(const Q4Args A, i
     store(A, A.first_token + n, h, v);
 }
 
-constexpr int wide_bytes = F_WARPS * WIDE_RING * WIDE_STAGE;
 template <int NT> constexpr int part_bytes = F_WARPS * NT * 512;
 template <int P, int NT, int GB> constexpr int grad_bytes = WARPS * (g_warp<P, NT, GB> > 8 * NT * COLS * 4 ? g_warp<P, NT, GB> : 8 * NT * COLS * 4);
 
 typedef void (*Kernel)(Q4Args);
-struct Variant { Kernel kernel; int smem, tokens, threads = F_THREADS; };
+struct Variant { Kernel kernel; int smem, tokens, threads; };
 
 // Forward: 8, 16 or 32 tokens to a block, the most (and no more than there are) whose inputs fit into shared memory
 // beside the rings; where those of 8 do not, they stay in global memory. Backward: 8 or 16.
+// The ring of a warp has three stages, or two where the tokens' fragments fit with two only (16 tokens of 4096 columns,
+// 32000 rows: 26 us, and 34 eight at a time).
+constexpr int SMEM_MOST = 226 * 1024;                      // (and a little of fixed size)
 template <int P, int NT, int GB, bool XS>
 Variant forward_kernel(int32_t H)
 {
-    return {od_q4_kernel<P, NT, GB, XS>, wide_bytes + part_bytes<NT> + H / GB * NT + (XS ? H * 16 * NT * P : 0), 8 * NT};
+    const int rest = part_bytes<NT> + H / GB * NT + (XS ? H * 16 * NT * P : 0), stage = F_WARPS * WIDE_STAGE;
+    if (!XS || rest + 3 * stage <= SMEM_MOST) return {od_q4_kernel<P, NT, GB, XS, 3>, rest + 3 * stage, 8 * NT, F_THREADS};
+    return {od_q4_kernel<P, NT, GB, XS, XS ? 2 : 3>, rest + 2 * stage, 8 * NT, F_THREADS};
 }
-constexpr int SMEM_MOST = 226 * 1024;                      // (and a little of fixed size)
 template <int GB>
 Variant forward_of(bool f32, int N, int32_t H)
 {
@@ -770,14 +772,19 @@ cudaError_t launch(K kernel, dim3 grid, dim3 threads, int smem, bool pdl, cudaSt
 
 cudaError_t od_q4_prepare_device()
 {
+    Kernel done = nullptr;
+    // (every variant: these sizes reach one, two, four parts of 8 tokens, rings of three and two stages, and none in shared memory)
     for (int backward = 0; backward < 2; ++backward)
         for (int32_t G = 32; G <= 128; G *= 2)
             for (int f32 = 0; f32 < 2; ++f32)
-                for (int N = 8; N <= 64; N *= 2) {         // (64: none in shared memory)
-                    const Variant v = variant(backward, G, f32, N, N == 64 ? 65536 : 128);
-                    cudaError_t e = cudaFuncSetAttribute((const void *)v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST);
-                    if (e != cudaSuccess) return e;
-                }
+                for (int N = 8; N <= 32; N *= 2)
+                    for (int32_t H = 128; H <= 65536; H += H < 16384 ? 128 : 49152) {
+                        const Variant v = variant(backward, G, f32, N, H);
+                        if (v.kernel == done) continue;
+                        const cudaError_t e = cudaFuncSetAttribute((const void *)v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST);
+                        if (e != cudaSuccess) return e;
+                        done = v.kernel;
+                    }
     return cudaSuccess;
 }
 
