@@ -52,15 +52,11 @@ __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_grou
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ uint32_t lds32(uint32_t at)
 {
-    uint32_t v;
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-    return v;
+    return *(const uint32_t *)__cvta_shared_to_generic(at);
 }
 __device__ __forceinline__ uint4 lds128(uint32_t at)
 {
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
-    return v;
+    return *(const uint4 *)__cvta_shared_to_generic(at);
 }
 __device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b)
 {
@@ -537,124 +533,127 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
         cp_wait<G_RING - 2>();
         __syncwarp();
         fetch();
-        // both halves of the rows side by side, for what can run at the same time
-        float d[2][NT][4], e[2][4][GROUPS];
+        // of eight tokens both halves of the rows side by side, for what can run at the same time; of sixteen registers lack
+        constexpr int SIDE = NT == 1 ? 2 : 1;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
+        for (int base = 0; base < 2; base += SIDE) {
+            float d[SIDE][NT][4], e[SIDE][4][GROUPS];
 #pragma unroll
-            for (int q = 0; q < NT; ++q) {
-                const uint32_t at = get_d + slot + q * 8 * (PIECES * 16);
-                if constexpr (F32) {
-                    const uint4 v = lds128(at ^ (half << 6));
-                    d[half][q][0] = __uint_as_float(v.x); d[half][q][1] = __uint_as_float(v.y);
-                    d[half][q][2] = __uint_as_float(v.z); d[half][q][3] = __uint_as_float(v.w);
-                } else {
-                    uint2 v;
-                    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at ^ (half << 5)) : "memory");
-                    d[half][q][0] = od_bf16_lo(v.x); d[half][q][1] = od_bf16_hi(v.x);
-                    d[half][q][2] = od_bf16_lo(v.y); d[half][q][3] = od_bf16_hi(v.y);
-                }
-            }
-            float flat[4 * GROUPS];                        // [row][group]
+            for (int half = 0; half < SIDE; ++half) {
 #pragma unroll
-            for (int k = 0; k < GROUPS; ++k)
-                *(float4 *)(flat + 4 * k) = *(const float4 *)(scale_of + (flip * G_ROWS + half * 16 + 4 * t) * GROUPS + 4 * k);
-#pragma unroll
-            for (int k = 0; k < 4 * GROUPS; ++k) e[half][k / GROUPS][k % GROUPS] = flat[k];
-        }
-#pragma unroll
-        for (int i = 0; i < GROUPS; ++i) {
-            if (i * GB >= here) break;
-            uint64_t z[2][NT][2];                          // pairs of rows
-            float m = 0.f;
-#pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-                for (int q = 0; q < NT; ++q)
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        z[half][q][k] = f2_mul(f2_pack(d[half][q][2 * k], d[half][q][2 * k + 1]), f2_pack(e[half][2 * k][i], e[half][2 * k + 1][i]));
-                        float lo, hi;
-                        f2_unpack(z[half][q][k], lo, hi);
-                        m = max_nan(max_nan(m, fabsf(lo)), fabsf(hi));
+                for (int q = 0; q < NT; ++q) {
+                    const uint32_t at = get_d + slot + q * 8 * (PIECES * 16);
+                    if constexpr (F32) {
+                        const uint4 v = lds128(at ^ ((base + half) << 6));
+                        d[half][q][0] = __uint_as_float(v.x); d[half][q][1] = __uint_as_float(v.y);
+                        d[half][q][2] = __uint_as_float(v.z); d[half][q][3] = __uint_as_float(v.w);
+                    } else {
+                        const uint2 v = *(const uint2 *)__cvta_shared_to_generic(at ^ ((base + half) << 5));
+                        d[half][q][0] = od_bf16_lo(v.x); d[half][q][1] = od_bf16_hi(v.x);
+                        d[half][q][2] = od_bf16_lo(v.y); d[half][q][3] = od_bf16_hi(v.y);
                     }
-            if (__any_sync(0xFFFFFFFFu, !(m < INFINITY))) {
-                // too large to be scaled, infinite or NaN (or nothing, and the scale too large)
+                }
+                float flat[4 * GROUPS];                        // [row][group]
 #pragma unroll
-                for (int half = 0; half < 2; ++half)
+                for (int k = 0; k < GROUPS; ++k)
+                    *(float4 *)(flat + 4 * k) = *(const float4 *)(scale_of + (flip * G_ROWS + (base + half) * 16 + 4 * t) * GROUPS + 4 * k);
+#pragma unroll
+                for (int k = 0; k < 4 * GROUPS; ++k) e[half][k / GROUPS][k % GROUPS] = flat[k];
+            }
+#pragma unroll
+            for (int i = 0; i < GROUPS; ++i) {
+                if (i * GB >= here) break;
+                uint64_t z[SIDE][NT][2];                          // pairs of rows
+                float m = 0.f;
+#pragma unroll
+                for (int half = 0; half < SIDE; ++half)
 #pragma unroll
                     for (int q = 0; q < NT; ++q)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
+                        for (int k = 0; k < 2; ++k) {
+                            z[half][q][k] = f2_mul(f2_pack(d[half][q][2 * k], d[half][q][2 * k + 1]), f2_pack(e[half][2 * k][i], e[half][2 * k + 1][i]));
                             float lo, hi;
-                            f2_unpack(z[half][q][k / 2], lo, hi);
-                            const bool large = !(fabsf(k & 1 ? hi : lo) < INFINITY);
-                            float big = 0.f;
-                            if (large) {
-                                const int v = s * G_ROWS + half * 16 + 4 * t + k;      // (behind the last row the scale is zero)
-                                big = d[half][q][k] * (1.f / BACK) * __uint_as_float((uint32_t)A.scales[(size_t)v * n_groups + col / (32 * GB) + i] << 16);
-                                z[half][q][k / 2] = k & 1 ? f2_pack(lo, 0.f) : f2_pack(0.f, hi);
-                            }
-                            for (unsigned lanes = __ballot_sync(0xFFFFFFFFu, large); lanes; lanes &= lanes - 1) {
-                                const int src = __ffs(lanes) - 1, n = src >> 2, r = half * 16 + 4 * (src & 3) + k;
-                                const float f = __shfl_sync(0xFFFFFFFFu, big, src);
-                                const unsigned char *const row = smem + warp * g_warp<P, NT, GB> + slot + r * 64;
+                            f2_unpack(z[half][q][k], lo, hi);
+                            m = max_nan(max_nan(m, fabsf(lo)), fabsf(hi));
+                        }
+                if (__any_sync(0xFFFFFFFFu, !(m < INFINITY))) {
+                    // too large to be scaled, infinite or NaN (or nothing, and the scale too large)
 #pragma unroll
-                                for (int c = 2 * i * GB; c < 2 * (i + 1) * GB; ++c) {
-                                    // the byte of a lane's two columns of sum c
-                                    const int at = PAIRS ? c / 4 * 32 + 4 * g + c % 4 : c / 2 * 16 + 2 * g + c % 2;
-                                    const uint32_t byte = row[((at >> 4 ^ (r >> 2 & 3)) << 4) + (at & 15)];
-                                    const float lo = f * (float)((int)(byte & 15) - 8), hi = f * (float)((int)(byte >> 4) - 8) * 16.f;
-                                    if (2 * t == n) { acc[c][q][0] += lo; acc[c][q][2] += hi; }
-                                    if (2 * t + 1 == n) { acc[c][q][1] += lo; acc[c][q][3] += hi; }
+                    for (int half = 0; half < SIDE; ++half)
+#pragma unroll
+                        for (int q = 0; q < NT; ++q)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                float lo, hi;
+                                f2_unpack(z[half][q][k / 2], lo, hi);
+                                const bool large = !(fabsf(k & 1 ? hi : lo) < INFINITY);
+                                float big = 0.f;
+                                if (large) {
+                                    const int v = s * G_ROWS + (base + half) * 16 + 4 * t + k;      // (behind the last row the scale is zero)
+                                    big = d[half][q][k] * (1.f / BACK) * __uint_as_float((uint32_t)A.scales[(size_t)v * n_groups + col / (32 * GB) + i] << 16);
+                                    z[half][q][k / 2] = k & 1 ? f2_pack(lo, 0.f) : f2_pack(0.f, hi);
+                                }
+                                for (unsigned lanes = __ballot_sync(0xFFFFFFFFu, large); lanes; lanes &= lanes - 1) {
+                                    const int src = __ffs(lanes) - 1, n = src >> 2, r = (base + half) * 16 + 4 * (src & 3) + k;
+                                    const float f = __shfl_sync(0xFFFFFFFFu, big, src);
+                                    const unsigned char *const row = smem + warp * g_warp<P, NT, GB> + slot + r * 64;
+#pragma unroll
+                                    for (int c = 2 * i * GB; c < 2 * (i + 1) * GB; ++c) {
+                                        // the byte of a lane's two columns of sum c
+                                        const int at = PAIRS ? c / 4 * 32 + 4 * g + c % 4 : c / 2 * 16 + 2 * g + c % 2;
+                                        const uint32_t byte = row[((at >> 4 ^ (r >> 2 & 3)) << 4) + (at & 15)];
+                                        const float lo = f * (float)((int)(byte & 15) - 8), hi = f * (float)((int)(byte >> 4) - 8) * 16.f;
+                                        if (2 * t == n) { acc[c][q][0] += lo; acc[c][q][2] += hi; }
+                                        if (2 * t + 1 == n) { acc[c][q][1] += lo; acc[c][q][3] += hi; }
+                                    }
                                 }
                             }
-                        }
-            }
-            uint32_t b[2][NT][2][P];
-#pragma unroll
-            for (int half = 0; half < 2; ++half)
-#pragma unroll
-                for (int q = 0; q < NT; ++q)
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        eights[i][q] = f2_fma(z[half][q][k], f2_pack(0x1p-126f * 0.0625f, 0x1p-126f * 0.0625f), eights[i][q]);      // 8 times 2^-133
-                        uint64_t rest = z[half][q][k];
-#pragma unroll
-                        for (int p = 0; p < P; ++p) {
-                            float lo, hi;
-                            f2_unpack(rest, lo, hi);
-                            b[half][q][k][p] = halves(__float_as_uint(lo), __float_as_uint(hi), HIGH);
-                            if (p + 1 < P)
-                                rest = f2_add(rest, f2_pack(-__uint_as_float(__float_as_uint(lo) & 0xFFFF0000u), -__uint_as_float(__float_as_uint(hi) & 0xFFFF0000u)));
-                        }
-                    }
-            // four codes of a lane in each of four rows: two columns of two sums
-            auto product = [&](uint32_t w01, uint32_t w23, int half, int c) {
-                const uint32_t v01 = w01 >> 8, v23 = w23 >> 8;
-                const uint32_t a0[4] = {w01 & CODE, w01 & CODE16, w23 & CODE, w23 & CODE16};       // (rows 8 on are 16 times as much)
-                const uint32_t a1[4] = {v01 & CODE, v01 & CODE16, v23 & CODE, v23 & CODE16};
-#pragma unroll
-                for (int p = 0; p < P; ++p)
-#pragma unroll
-                    for (int q = 0; q < NT; ++q) {
-                        mma(acc[c][q], a0, b[half][q][0][p], b[half][q][1][p]);
-                        mma(acc[c + 1][q], a1, b[half][q][0][p], b[half][q][1][p]);
-                    }
-            };
-#pragma unroll
-            for (int j = i * GB; j < (i + 1) * GB; j += PAIRS ? 2 : 1)
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const uint32_t at = get + slot + half * 16 * 64 + ((PAIRS ? (j + (g >> 2)) ^ t : j ^ t) << 4);
-                    const uint32_t w0 = lds32(at), w1 = lds32(at + 64), w2 = lds32(at + 128), w3 = lds32(at + 192);
-                    if constexpr (PAIRS) {
-                        product(halves(w0, w1, LOW), halves(w2, w3, LOW), half, 2 * j);
-                        product(halves(w0, w1, HIGH), halves(w2, w3, HIGH), half, 2 * j + 2);
-                    } else {
-                        product(halves(w0, w1, pick), halves(w2, w3, pick), half, 2 * j);
-                    }
                 }
+                uint32_t b[SIDE][NT][2][P];
+#pragma unroll
+                for (int half = 0; half < SIDE; ++half)
+#pragma unroll
+                    for (int q = 0; q < NT; ++q)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            eights[i][q] = f2_fma(z[half][q][k], f2_pack(0x1p-126f * 0.0625f, 0x1p-126f * 0.0625f), eights[i][q]);      // 8 times 2^-133
+                            uint64_t rest = z[half][q][k];
+#pragma unroll
+                            for (int p = 0; p < P; ++p) {
+                                float lo, hi;
+                                f2_unpack(rest, lo, hi);
+                                b[half][q][k][p] = halves(__float_as_uint(lo), __float_as_uint(hi), HIGH);
+                                if (p + 1 < P)
+                                    rest = f2_add(rest, f2_pack(-__uint_as_float(__float_as_uint(lo) & 0xFFFF0000u), -__uint_as_float(__float_as_uint(hi) & 0xFFFF0000u)));
+                            }
+                        }
+                // four codes of a lane in each of four rows: two columns of two sums
+                auto product = [&](uint32_t w01, uint32_t w23, int half, int c) {
+                    const uint32_t v01 = w01 >> 8, v23 = w23 >> 8;
+                    const uint32_t a0[4] = {w01 & CODE, w01 & CODE16, w23 & CODE, w23 & CODE16};       // (rows 8 on are 16 times as much)
+                    const uint32_t a1[4] = {v01 & CODE, v01 & CODE16, v23 & CODE, v23 & CODE16};
+#pragma unroll
+                    for (int p = 0; p < P; ++p)
+#pragma unroll
+                        for (int q = 0; q < NT; ++q) {
+                            mma(acc[c][q], a0, b[half][q][0][p], b[half][q][1][p]);
+                            mma(acc[c + 1][q], a1, b[half][q][0][p], b[half][q][1][p]);
+                        }
+                };
+#pragma unroll
+                for (int j = i * GB; j < (i + 1) * GB; j += PAIRS ? 2 : 1)
+#pragma unroll
+                    for (int half = 0; half < SIDE; ++half) {
+                        const uint32_t at = get + slot + (base + half) * 16 * 64 + ((PAIRS ? (j + (g >> 2)) ^ t : j ^ t) << 4);
+                        const uint32_t w0 = lds32(at), w1 = lds32(at + 64), w2 = lds32(at + 128), w3 = lds32(at + 192);
+                        if constexpr (PAIRS) {
+                            product(halves(w0, w1, LOW), halves(w2, w3, LOW), half, 2 * j);
+                            product(halves(w0, w1, HIGH), halves(w2, w3, HIGH), half, 2 * j + 2);
+                        } else {
+                            product(halves(w0, w1, pick), halves(w2, w3, pick), half, 2 * j);
+                        }
+                    }
+            }
         }
         slot = slot + STAGE == G_RING * STAGE ? 0 : slot + STAGE;
         flip ^= 1;
