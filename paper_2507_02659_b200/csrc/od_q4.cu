@@ -149,25 +149,29 @@ struct Scales {
 // Nothing is subtracted from the codes, and nothing is or'ed to them: the 8 bits of a code u, or of 16 u, are the bf16 number
 // u 2^-133, or 16 u 2^-133 (with no more bits set a bf16 is its bits times 2^-133, in the first binade too). So two masks,
 // a shift and two masks unpack a word; inputs that meet a 16 u are divided by 16. For products in fp32's range a token is
-// scaled by a power of two that brings its largest magnitude to 2^126, and its sums are scaled back at the end. The 8 that is
+// scaled by a power of two, and its sums are scaled back at the end. The 8 that is
 // left out is in what a group's sum begins at: -8 times the sum of its inputs, in the same units. It adds to the sums'
 // magnitudes no more than their codes do. (With 136 subtracted from bf16 numbers 128 + u in the loop: 59 us where it
 // is 45, eight tokens through 128256 x 4096.)
 
-// eight columns of a token (columns 8t .. 8t + 7 of a block), scaled; a token with infinities or NaN is zero here
+// The scale of a token whose largest magnitude has these bits is 2^k: 66 for nearly all, whose products then are x u 2^-67; of
+// the very large and the very small (all of them zero too) what brings the largest to 2^126.
+__device__ __forceinline__ bool usual(uint32_t largest) { return largest >= (127u - 30 << 23) && largest < (127u + 60 << 23); }
+__device__ __forceinline__ int scale_of_token(uint32_t largest) { return usual(largest) ? 66 : 253 - (int)(largest >> 23); }
+// eight columns of a token (columns 8t .. 8t + 7 of a block) by this; a token with infinities or NaN is zero here
 struct Token {
     float up, up2;                                         // the scale is their product
-    __device__ __forceinline__ Token(uint32_t largest)     // bits of the largest magnitude
+    __device__ __forceinline__ Token(uint32_t largest)
     {
-        const int e = largest >> 23, k = e < 255 ? 253 - e : 0, h = k / 2;
-        up = e < 255 ? __int_as_float((127 + h) << 23) : 0.f;
+        const int k = largest < 0x7F800000u ? scale_of_token(largest) : 0, h = k / 2;
+        up = largest < 0x7F800000u ? __int_as_float((127 + h) << 23) : 0.f;
         up2 = __int_as_float((127 + k - h) << 23);
     }
 };
 // sums of a token back to its units: they are of products times 2^(k - 133)
 __device__ __forceinline__ float scaled_back(float v, uint32_t largest)
 {
-    const int e = largest >> 23, k = 133 - (253 - e), h = k / 2;
+    const int k = 133 - scale_of_token(largest), h = k / 2;
     return v * __int_as_float((127 + h) << 23) * __int_as_float((127 + k - h) << 23);
 }
 template <bool F32>
@@ -224,7 +228,7 @@ template <int P, int NT, int GB, bool XS, int RING>
 __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
 {
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ uint32_t largest_of[8 * NT][2];
+    __shared__ uint32_t largest_of[8 * NT];                // bits of the tokens' largest magnitudes
     constexpr bool F32 = P == 3;
     constexpr int IN_BYTES = F32 ? 4 : 2;
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -263,48 +267,48 @@ __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
 #pragma unroll
     for (int i = 0; i < RING - 1; ++i) fetch();
 
-    // the largest magnitude of each token, by two warps
-    for (int i = warp; i < 16 * NT; i += F_WARPS) {
-        const int n = n0 + i / 2;
-        const char *at = (const char *)A.in + (int64_t)(n < A.N ? n : 0) * A.in_stride * IN_BYTES;
-        uint32_t m = 0;
-        for (int k = (i & 1) * 32 + lane; k < H * IN_BYTES / 16; k += 64) {
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (n < A.N) v = __ldg((const uint4 *)at + k);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) m = F32 ? max(m, w[j] & 0x7FFFFFFFu) : max(m, max(w[j] & 0x7FFF0000u, w[j] << 16 & 0x7FFFFFFFu));
-        }
-        m = __reduce_max_sync(0xFFFFFFFFu, m);
-        if (lane == 0) largest_of[i / 2][i & 1] = m;
-    }
-    __syncthreads();
-    auto largest = [&](int n) { return max(largest_of[n][0], largest_of[n][1]); };
-
     // [group][8 tokens to a part]: what the group's sums begin at; [block of 32 columns][part][piece][lane]: the fragments
     float *const starts = (float *)(smem + F_WARPS * RING * WIDE_STAGE);
     unsigned char *const inputs = (unsigned char *)(starts + n_groups * 8 * NT);
-    for (int i = warp; i < n_groups * NT; i += F_WARPS) {
-        const int q = i % NT, n = n0 + q * 8 + g;
-        const Token k(largest(q * 8 + g));
-        float start = 0.f;
+    auto prepare = [&](bool all_usual) {
+        for (int i = warp; i < n_groups * NT; i += F_WARPS) {
+            const int q = i % NT, n = n0 + q * 8 + g;
+            const Token k(all_usual ? 127u << 23 : largest_of[q * 8 + g]);
+            float start = 0.f;
+            uint32_t m = 0;
 #pragma unroll
-        for (int j = 0; j < GB; ++j) {
-            const int blk = i / NT * GB + j;
-            float x[8];
-            load_columns<F32>((const char *)A.in + ((int64_t)n * A.in_stride + blk * 32 + t * 8) * IN_BYTES, n < A.N, x);
-            uint32_t b[P][4];
-            cut_columns<P>(x, k, b);
+            for (int j = 0; j < GB; ++j) {
+                const int blk = i / NT * GB + j;
+                float x[8];
+                load_columns<F32>((const char *)A.in + ((int64_t)n * A.in_stride + blk * 32 + t * 8) * IN_BYTES, n < A.N, x);
+                if (all_usual)
 #pragma unroll
-            for (int c = 0; c < 8; ++c) start = fmaf(x[c], -0x1p-126f * 0.0625f, start);       // -8 times 2^-133
-            if constexpr (XS)
+                    for (int c = 0; c < 8; ++c) m = max(m, __float_as_uint(x[c]) & 0x7FFFFFFFu);
+                uint32_t b[P][4];
+                cut_columns<P>(x, k, b);
 #pragma unroll
-                for (int p = 0; p < P; ++p) ((uint4 *)inputs)[((blk * NT + q) * P + p) * 32 + lane] = make_uint4(b[p][0], b[p][1], b[p][2], b[p][3]);
+                for (int c = 0; c < 8; ++c) start = fmaf(x[c], -0x1p-126f * 0.0625f, start);   // -8 times 2^-133
+                if constexpr (XS)
+#pragma unroll
+                    for (int p = 0; p < P; ++p) ((uint4 *)inputs)[((blk * NT + q) * P + p) * 32 + lane] = make_uint4(b[p][0], b[p][1], b[p][2], b[p][3]);
+            }
+            start += __shfl_xor_sync(0xFFFFFFFFu, start, 1);
+            start += __shfl_xor_sync(0xFFFFFFFFu, start, 2);
+            if (t == 0) starts[i * 8 + g] = start;
+            if (all_usual) {
+                m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+                m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
+                if (t == 0) atomicMax(&largest_of[q * 8 + g], m);
+            }
         }
-        start += __shfl_xor_sync(0xFFFFFFFFu, start, 1);
-        start += __shfl_xor_sync(0xFFFFFFFFu, start, 2);
-        if (t == 0) starts[i * 8 + g] = start;
-    }
+    };
+    if (threadIdx.x < 8 * NT) largest_of[threadIdx.x] = 0;
+    __syncthreads();
+    prepare(true);
+    // (a token of zeros is as good with any scale)
+    __syncthreads();
+    if (__syncthreads_or(threadIdx.x < 8 * NT && largest_of[threadIdx.x] != 0 && !usual(largest_of[threadIdx.x]))) prepare(false);
+    auto largest = [&](int n) { return largest_of[n]; };
     const char *x_at[NT];
     if constexpr (!XS)
 #pragma unroll
