@@ -457,8 +457,10 @@ int32_t od_token_logprobs_grad(od_ctx *ctx, int32_t B, int32_t R, int32_t vocab,
  *   w[v,h] = scales[v, h / group] * (code[v,h] - 8),
  *   logits[n,v] = sum_h hidden[n,h] w[v,h],   g_hidden[n,h] = sum_v g_logits[n,v] w[v,h].
  * Sums are fp32, nothing is rounded before them: a product of an input and a code is exact, scales
- * are applied to sums over a group (logits; such a sum has to stay within fp32's range) or to the
- * input (gradient, one fp32 rounding).
+ * are applied to sums over a group (logits) or to the input (gradient, one fp32 rounding). Infinities
+ * and NaN of the inputs give what the formula gives; scales are finite. (Digits go lost, as in fp32's
+ * smallest numbers, of hidden states below 2^-90 of their token's largest and of gradient times scale
+ * below 2^-103.)
  *   in  (device) hidden / g_logits fp32 or bf16, N rows, row stride in elements, base and stride
  *                multiples of 16 bytes
  *                codes  uint8[vocab, hidden_size / 2], dense, 16-byte aligned: column 2i of a row in
@@ -468,8 +470,10 @@ int32_t od_token_logprobs_grad(od_ctx *ctx, int32_t B, int32_t R, int32_t vocab,
  *   out (device) logits / g_hidden fp32 or bf16, N rows, base and stride multiples of 16 bytes;
  *                nothing behind a row is written
  * Neither vocab nor N is bound to the context. Made for N up to some dozens of tokens: the weights are
- * unpacked again for every few of them. Asynchronous on `stream`; no scratch, the same results in
- * every run. */
+ * unpacked again for every few of them. Asynchronous on `stream`, allocates nothing, the same results
+ * in every run. od_q4_logits_grad joins its sums in the context's scratch: it is ordered with the
+ * other calls of its kind on the context like the step functions (graphs that hold it too);
+ * od_q4_logits has no scratch. */
 int32_t od_q4_logits(od_ctx *ctx, int32_t N, int32_t vocab, int32_t hidden_size, int32_t group,
                      const void *hidden, int32_t hidden_dtype, int64_t hidden_stride,
                      const void *codes, const void *scales, void *logits, int32_t logit_dtype,

@@ -207,15 +207,15 @@ PyObject *distill_loss(PyObject *, PyObject *const *a, Py_ssize_t n)
     return call(x, od_distill_loss, args);
 }
 
-// rows [B, R, V] (or [N, V] as one sequence) with dense rows of whole 16-byte strides, in their order
+// rows [B, R, V] (where sequences do not matter [N, V] too, as one) with dense rows of whole 16-byte strides, in their order
 struct Rows {
     void *p = nullptr;
     int32_t dtype = 0;
     int64_t B = 0, R = 0, V = 0, row_stride = 0, seq_stride = 0;
-    Rows(Args &x, const at::Tensor *t)
+    Rows(Args &x, const at::Tensor *t, bool sequences)
     {
         const int64_t d = t ? t->dim() : 0;
-        if ((d != 2 && d != 3) || t->numel() == 0 || (t->size(d - 1) > 1 && t->stride(d - 1) != 1) ||
+        if ((d != 3 && (d != 2 || sequences)) || t->numel() == 0 || (t->size(d - 1) > 1 && t->stride(d - 1) != 1) ||
             (t->scalar_type() != c10::kFloat && t->scalar_type() != c10::kBFloat16)) {
             x.ok = false;
             return;
@@ -250,7 +250,7 @@ PyObject *token_logprobs(PyObject *, PyObject *const *a, Py_ssize_t n)
     Args x(a, n, 14);
     od_ctx *c = x.ctx();
     const int32_t n_top = x.i32();
-    const Rows l(x, x.tensor());
+    const Rows l(x, x.tensor(), true);
     const int64_t br[] = {l.B, l.R}, top[] = {l.B, l.R, n_top}, b[] = {l.B};
     const int32_t *ids = shaped<int32_t>(x, c10::kInt, br, true);
     const float *T = shaped<float>(x, c10::kFloat, b, true);
@@ -269,7 +269,7 @@ PyObject *token_logprobs_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     Args x(a, n, 14);
     od_ctx *c = x.ctx();
-    const Rows l(x, x.tensor());
+    const Rows l(x, x.tensor(), true);
     const int64_t br[] = {l.B, l.R}, b[] = {l.B};
     const int32_t *ids = shaped<int32_t>(x, c10::kInt, br, true);
     const float *T = shaped<float>(x, c10::kFloat, b, true);
@@ -278,7 +278,7 @@ PyObject *token_logprobs_grad(PyObject *, PyObject *const *a, Py_ssize_t n)
     const at::Tensor *top_ids = x.tensor();
     const float *g_lp = shaped<float>(x, c10::kFloat, br, true), *g_h = shaped<float>(x, c10::kFloat, br, true);
     const at::Tensor *g_top = x.tensor(true);
-    const Rows g(x, x.tensor());
+    const Rows g(x, x.tensor(), true);
     if (g.B != l.B || g.R != l.R || g.V != l.V || g.dtype != l.dtype) x.ok = false;
     int32_t n_top = 0;
     if (x.ok && g_top) {
@@ -302,9 +302,9 @@ PyObject *q4(PyObject *, PyObject *const *a, Py_ssize_t n)
     Args x(a, n, 6);
     od_ctx *c = x.ctx();
     const at::Tensor *in_t = x.tensor();
-    const Rows in(x, in_t);
+    const Rows in(x, in_t, false);
     const at::Tensor *codes = x.tensor(), *scales = x.tensor(), *out_t = x.tensor();
-    const Rows out(x, out_t);
+    const Rows out(x, out_t, false);
     if (!x.ok || codes->dim() != 2 || scales->dim() != 2 || codes->scalar_type() != c10::kByte || scales->scalar_type() != c10::kBFloat16 ||
         !codes->is_contiguous() || !scales->is_contiguous())
         Py_RETURN_NONE;

@@ -3,18 +3,28 @@
 // Codes u are 4 bits (column 2i in the low half of byte i of a row), scales s are bf16.
 //
 // Both products run on the tensor pipe as mma.m16n8k16 with the codes as the first operand and eight tokens as the
-// second. u - 8 is exact in bf16, and so is an input: a bf16 one as it is, an fp32 one as the sum of three bf16 pieces
+// second. A code is exact in bf16, and so is an input: a bf16 one as it is, an fp32 one as the sum of three bf16 pieces
 // (24 bits = 8 + 8 + 8), the product of a bf16 gradient and a bf16 scale as that of two. So the only roundings are those
 // of fp32 sums (and of an fp32 gradient times its scale). The scale of a group belongs to a row of the weights: forward
 // it multiplies the group's sum, backward, where rows are summed over, the gradient.
 //
-// For a few tokens the codes are all there is to move; what competes with them is unpacking: 11 instructions for eight
-// codes (three shifts, four masks that put a code into the low mantissa bits of bf16 128, four subtractions of 136).
-// That is why the operands go from registers straight into mma.sync and not through shared memory to tcgen05, whose
-// operands would be written and read there once more at two bytes a weight.
+// For a few tokens the codes are all there is to move, and unpacking them is what competes with that. Nothing is subtracted
+// from a code and nothing or'ed to it: with no more than eight bits set a bf16 number is its bits times 2^-133 (in the first
+// binade too), so two masks, a shift and two masks make eight codes u, half of them as 16 u, ready for the tensor pipe. The
+// inputs are scaled by a power of two so that products are in fp32's range, and where a 16 u meets an input that one is
+// divided by 16 (forward) or the result is (backward). The 8 is taken off in sums: of a group's inputs (forward, where the
+// group's sum begins), of all scaled gradients (backward, at the end). It adds no more to the sums' magnitudes than the
+// codes do. (Eight tokens through 128256 x 4096: 59 us with 136 subtracted from bf16 numbers 128 + u, 52 us so.)
+// Operands go from registers into mma.sync: for tcgen05 they would be written to shared memory and read there at two
+// bytes a weight, 29 us of its bandwidth for 128256 x 2048, whose codes HBM brings in 21.
 //
-// A warp streams its own codes through a ring of 1 KB stages in shared memory (16 rows x 128 columns, cp.async), so that
-// no block barrier holds it up; sixteen-byte pieces are placed so that the words of a fragment lie in different banks.
+// A warp streams its own codes through a ring in shared memory (cp.async, 2 KB stages), so that no block barrier holds it
+// up: without the arithmetic the forward kernel reads 6.2 TB/s. Sixteen-byte pieces are placed so that the words of a
+// fragment lie in different banks.
+//
+// Measured (us; codes and scales / HBM's rate): forward 8 tokens, 128256 x 4096 in groups of 128: 52 (42); backward 8
+// positions, 128256 x 2048: 42 (21), 16: 62. What bounds both now is issue: masks share their dispatch with the matrix
+// instructions (ncu: masks' pipe 58 %, tensor pipe 31 % forward; 56 % and 40 % backward).
 #include <float.h>
 
 #include "od_common.cuh"
@@ -27,7 +37,7 @@ constexpr int ROWS = 16;                                   // of a matrix instru
 constexpr int COLS = 128;                                  // backward: of a warp, four blocks of 32
 constexpr int G_RING = 3;                                  // backward: stages of a warp
 constexpr int WIDE = 8;                                    // forward: blocks of 32 columns to a stage
-constexpr int WIDE_STAGE = ROWS * WIDE * 16;
+constexpr int WIDE_STAGE = ROWS * WIDE * 16;              // bytes
 
 struct Q4Args {
     const void *in;                                        // x or dy
@@ -146,18 +156,11 @@ struct Scales {
 // a token. XS: a block of threads keeps its tokens' inputs in shared memory as the words of the fragments, 16 bytes to a
 // lane; where they do not fit, they are read and cut again for every 16 rows.
 
-// Nothing is subtracted from the codes, and nothing is or'ed to them: the 8 bits of a code u, or of 16 u, are the bf16 number
-// u 2^-133, or 16 u 2^-133 (with no more bits set a bf16 is its bits times 2^-133, in the first binade too). So two masks,
-// a shift and two masks unpack a word; inputs that meet a 16 u are divided by 16. For products in fp32's range a token is
-// scaled by a power of two, and its sums are scaled back at the end. The 8 that is
-// left out is in what a group's sum begins at: -8 times the sum of its inputs, in the same units. It adds to the sums'
-// magnitudes no more than their codes do. (With 136 subtracted from bf16 numbers 128 + u in the loop: 59 us where it
-// is 45, eight tokens through 128256 x 4096.)
-
-// The scale of a token whose largest magnitude has these bits is 2^k: 66 for nearly all, whose products then are x u 2^-67; of
-// the very large and the very small (all of them zero too) what brings the largest to 2^126.
-__device__ __forceinline__ bool usual(uint32_t largest) { return largest >= (127u - 30 << 23) && largest < (127u + 60 << 23); }
-__device__ __forceinline__ int scale_of_token(uint32_t largest) { return usual(largest) ? 66 : 253 - (int)(largest >> 23); }
+// The scale of a token whose largest magnitude has these bits is 2^k: 106 where that is from 2^-8 up to 2^20, as it is nearly
+// always, so that products are x u 2^-27; for others (all of zeros too) what brings the largest to 2^126. An input keeps all its
+// digits down to 2^-90 of its token's largest.
+__device__ __forceinline__ bool usual(uint32_t largest) { return largest >= (127u - 8 << 23) && largest < (127u + 20 << 23); }
+__device__ __forceinline__ int scale_of_token(uint32_t largest) { return usual(largest) ? 106 : 253 - (int)(largest >> 23); }
 // eight columns of a token (columns 8t .. 8t + 7 of a block) by this; a token with infinities or NaN is zero here
 struct Token {
     float up, up2;                                         // the scale is their product

@@ -650,12 +650,12 @@ cudaError_t od_launch_score(const od_ctx *c, int32_t B, int32_t R, int32_t V, co
 {
     const int64_t esz = dtype == OD_BF16 ? 2 : 4, rows = (int64_t)B * R;
     // Blocks of a row: one for many rows, up to 8 where there are few (of ragged ones half count, about): at most seven for two
-    // multiprocessors, and none of a slice below 16 KB. (us with 20 alternatives, 1 / 2 / 4 / 8 blocks a row: one row of
+    // multiprocessors, and none of a slice below 14 KB. (us with 20 alternatives, 1 / 2 / 4 / 8 blocks a row: one row of
     // 152064 bf16 logits 21 / 14 / 11 / 10, 96 rows of 128256 19 / 16 / 16 / 21, 448 rows 39 / 40 / 48 / 70, 4608 rows of
     // 152064 290 / 345 / 461 / 738.)
     const int64_t count = n_rows ? (rows + 1) / 2 : rows;
     int32_t split = 1;
-    while (split < MAX_SPLIT && count * split * 4 <= 7 * c->sm_count && (int64_t)V * esz / (split * 2) >= 16384 - 256) split *= 2;
+    while (split < MAX_SPLIT && count * split * 4 <= 7 * c->sm_count && (int64_t)V * esz / (split * 2) >= 14 * 1024) split *= 2;
     const ScoreArgs a = {(const char *)logits, row_stride * esz, seq_stride * esz, R, V, n_top, split, ids, n_rows, temperature,
                          logprob, entropy, row_max, row_sum, top_logprobs, top_ids, flags};
     const unsigned blocks = (unsigned)(rows * split);

@@ -286,3 +286,102 @@ def test_refusals(ctx):
     assert e.value.status == od.OD_ERR_ALIGNMENT
     assert od.od_q4_logits(ctx, x[:0], codes, scales).shape == (0, 100)
     assert od.od_q4_logits_grad(ctx, torch.zeros(0, 100, device="cuda"), codes, scales).shape == (0, 128)
+
+
+def test_scales_far_from_one(ctx):
+    """Scales that cannot be scaled up with the rest, and tiny ones, next to usual ones: groups of either kind in both directions."""
+    N, V, H, G = 9, 70, 256, 64
+    codes, scales = layer(V, H, G, 20)
+    power = torch.tensor([0.0, 90.0, -90.0, 1.0], device="cuda")
+    scales = (scales.double() * 2.0 ** power[None, :]).to(BF16)
+    scales[5, 0], scales[6, 1] = 2.0 ** 70, 0.0
+    x = torch.randn(N, H, device="cuda")
+    x[:, G:2 * G] *= 2.0 ** -80
+    x[3] = 0.0
+    for dtype in (BF16, F32):
+        xd = x.to(dtype)
+        check_logits(od.od_q4_logits(ctx, xd, codes, scales), xd, weights(codes, scales), G, magnitudes(codes, scales))
+    dy = torch.randn(N, V, device="cuda") * 2.0 ** -20
+    dy[2] = 0.0
+    for dtype in (BF16, F32):
+        d = padded(dy.to(dtype))
+        check_grad(od.od_q4_logits_grad(ctx, d, codes, scales), d, weights(codes, scales), magnitudes(codes, scales))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_tokens_of_all_sizes_in_one_call(ctx, dtype):
+    """Tokens of usual size, tiny, huge, all zeros and not finite beside one another."""
+    N, V, H, G = 16, 100, 512, 128
+    codes, scales = layer(V, H, G, 21)
+    g = torch.Generator(device="cuda").manual_seed(22)
+    x = torch.randn(N, H, generator=g, device="cuda", dtype=torch.float64)
+    x *= 2.0 ** torch.tensor([0, -100, 90, 0, 59, 60, -30, -31, -126, 1, 20, -20, 0, 0, 3, -3.0], device="cuda", dtype=torch.float64)[:, None]
+    x[3] = 0.0
+    x = x.to(dtype)
+    x[12, 7] = math.inf
+    y = od.od_q4_logits(ctx, x, codes, scales)
+    keep = [n for n in range(N) if n != 12]
+    w, size_of = weights(codes, scales), magnitudes(codes, scales)
+    check_logits(y[[n for n in keep if n != 8]], x[[n for n in keep if n != 8]], w, G, size_of)
+    # (the least one's results are of the size of fp32's smallest numbers, 2^-149 apart)
+    want = x[8].double() @ w.T
+    assert ((y[8].double() - want).abs() <= x[8].double().abs() @ size_of.T * 2.0 ** -17 + 2.0 ** -148).all()
+    assert not torch.isfinite(y[12][w[:, 7] != 0]).any()
+    assert torch.equal(od.od_q4_logits(ctx, x[:1], codes, scales), od.od_q4_logits(ctx, x[:2], codes, scales)[:1])
+
+
+def test_many_tokens(ctx):
+    N, V, H, G = 131, 300, 384, 128
+    codes, scales = layer(V, H, G, 23)
+    w, size_of = weights(codes, scales), magnitudes(codes, scales)
+    x, dy = torch.randn(N, H, device="cuda").to(BF16), padded(torch.randn(N, V, device="cuda").to(BF16))
+    check_logits(od.od_q4_logits(ctx, x, codes, scales), x, w, G, size_of)
+    check_grad(od.od_q4_logits_grad(ctx, dy, codes, scales), dy, w, size_of)
+
+
+def test_two_streams_at_once(ctx):
+    """od_q4_logits has no scratch: calls on one context need no order."""
+    V, H, G = 20000, 1024, 64
+    codes, scales = layer(V, H, G, 24)
+    xs = [torch.randn(n, H, device="cuda").to(BF16) for n in (3, 20)]
+    want = [od.od_q4_logits(ctx, x, codes, scales) for x in xs]
+    out = [torch.zeros_like(y) for y in want]
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for x, y, s in zip(xs, out, streams):
+            with torch.cuda.stream(s):
+                od.od_q4_logits(ctx, x, codes, scales, out=y)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+def test_with_and_without_the_extension(ctx, monkeypatch):
+    codes, scales = layer(100, 128, 32, 25)
+    x, dy = torch.randn(2, 3, 128, device="cuda"), padded(torch.randn(2, 3, 100, device="cuda"))
+    y, dx = torch.empty(2, 3, 100, device="cuda"), torch.empty(2, 3, 128, device="cuda")
+    a = od.od_q4_logits(ctx, x, codes, scales, out=y).clone(), od.od_q4_logits_grad(ctx, dy, codes, scales, out=dx).clone()
+    monkeypatch.setattr(od, "_native", od._InPython())
+    b = od.od_q4_logits(ctx, x, codes, scales, out=y), od.od_q4_logits_grad(ctx, dy, codes, scales, out=dx)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_the_distillation_gradient_back_to_the_hidden_states(ctx):
+    """A verified batch's distillation loss, its gradient and the drafter's 4-bit layer: d loss / d hidden against 64 bits."""
+    from paper_2507_02659_b200 import synth
+    import parity
+    V_q, H, G = 1200, 256, 64
+    w = synth.Workload("q4distill", B=4, steps=1, k_max=4, k_min=1, v_q=V_q, v_p=5003, logit_dtype="bf16", map_kind="random",
+                       mapped_frac=0.7, cache_entries=100, hit_prob=0.3, logit_kind="corr", rho=0.95, temperatures=(1.0, 0.5),
+                       per_seq_seed=True, gen_seed=0x5C1, unmapped_shift=2.0, sigma=2.0)
+    st = synth.make_static(w)
+    c = parity.make_context(w, st, "cuda:0")
+    s = synth.make_step(w, st, 0, device="cuda:0")
+    logits = parity.pad_rows(s.logits)
+    mp = od.od_map_proposals(c, s.draft_ids, s.draft_len, s.q_sel)
+    vo = od.od_verify(c, logits, mp, s.temperature, s.seed, 0)
+    _, grad = od.od_distill_loss(c, s.q_rows, s.draft_ids, mp, logits, vo, s.temperature, 0.2)
+    codes, scales = layer(V_q, H, G, 26)
+    got = od.od_q4_logits_grad(c, grad, codes, scales)
+    check_grad(got.view(-1, H), grad.view(-1, V_q), weights(codes, scales), magnitudes(codes, scales))
+    c.close()

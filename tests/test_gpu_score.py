@@ -386,6 +386,45 @@ def test_scores_of_a_step(ctx):
     c.close()
 
 
+def test_long_rows_of_many(ctx):
+    """A block to a row and more turns of a thread than it leaves maxima."""
+    B, V, n = 300, 300007, 20
+    x, ids, T = make(B, 1, V, torch.bfloat16, 15)
+    out = od.od_token_logprobs(ctx, x, ids, T, n_top=n)
+    for lo in (0, B - 8):
+        ref = reference(x[lo:lo + 8], ids[lo:lo + 8], T[lo:lo + 8], n)
+        check(od.LogprobOut(*(t[lo:lo + 8] for t in vars(out).values())), ref, n)
+
+
+def test_two_streams_at_once(ctx):
+    """No scratch: calls on one context need no order."""
+    cases = [make(b, r, v, torch.bfloat16, 16) for b, r, v in ((1, 1, 152064), (40, 4, 32000))]
+    want = [vars(od.od_token_logprobs(ctx, x, ids, T, n_top=7)) for x, ids, T in cases]
+    outs = [od.alloc_logprob_out(ctx, x.shape[0], x.shape[1], 7) for x, _, _ in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for (x, ids, T), out, s in zip(cases, outs, streams):
+            with torch.cuda.stream(s):
+                od.od_token_logprobs(ctx, x, ids, T, n_top=7, out=out)
+    torch.cuda.synchronize()
+    for w, out in zip(want, outs):
+        assert all(torch.equal(w[k], t) for k, t in vars(out).items())
+
+
+def test_with_and_without_the_extension(ctx, monkeypatch):
+    x, ids, T = make(3, 4, 777, torch.float32, 17)
+    n_rows = torch.tensor([1, 4, 2], dtype=torch.int32, device="cuda")
+    one, g_top = torch.ones(3, 4, device="cuda"), torch.ones(3, 4, 5, device="cuda")
+
+    def both():
+        out = od.od_token_logprobs(ctx, x, ids, T, n_rows, 5, out=od.alloc_logprob_out(ctx, 3, 4, 5))
+        return [*vars(out).values(), od.od_token_logprobs_grad(ctx, x, ids, out, one, one, g_top, T, n_rows, grad=padded(x))]
+    a = both()
+    monkeypatch.setattr(od, "_native", od._InPython())
+    assert all(torch.equal(p, q) for p, q in zip(a, both()))
+
+
 def test_refusals(ctx):
     x, ids, T = make(2, 3, 64, torch.bfloat16, 14)
     out = od.od_token_logprobs(ctx, x, ids, T, n_top=2)
@@ -415,5 +454,7 @@ def test_refusals(ctx):
         od.od_token_logprobs_grad(ctx, x, ids, out, out.logprob, grad=torch.empty(2, 3, 64, device="cuda"))
     with pytest.raises(ValueError):
         od.od_token_logprobs_grad(ctx, x, ids, out, out.logprob, g_top=torch.zeros(2, 3, 5, device="cuda"))
+    with pytest.raises(ValueError):                         # rows without sequences
+        od.od_token_logprobs(ctx, x[0], ids[:1], T[:1], n_top=2, out=od.alloc_logprob_out(ctx, 1, 3, 2))
     assert od.od_token_logprobs(ctx, x[:0], ids[:0], T[:0], n_top=2).logprob.shape == (0, 3)
     np.testing.assert_array_equal(od.od_token_logprobs(ctx, x, ids, T, n_top=2).top_ids.cpu(), out.top_ids.cpu())
