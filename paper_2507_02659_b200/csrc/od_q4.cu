@@ -50,6 +50,7 @@ struct Q4Args {
     int32_t wide_scales;                                   // the scales of a stage's row are one aligned word
     int32_t k_split;                                       // forward: warps to the same rows
     int32_t split, col_warps;                              // backward: blocks on the same columns, warps side by side
+    int32_t cluster;                                       // the blocks on the same columns are one
     int32_t first_token;
     float *parts;                                          // the context's scratch
 };
@@ -73,6 +74,12 @@ __device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b)
     uint64_t d;
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
+}
+__device__ __forceinline__ float load_cluster(const float *p, uint32_t rank)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(od_cluster_address(p, rank)) : "memory");
+    return v;
 }
 __device__ __forceinline__ float max_nan(float a, float b)
 {
@@ -442,8 +449,8 @@ __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
 // what is too large for that (and infinities and NaN) is added to the sums on its own. The 8 of a code is taken off at the
 // end: sums of gradient times scale, of which a lane has those of its rows.
 // Warps side by side share rows (a block reads up to 256 bytes in a row). Those on the same columns are summed at the end,
-// and the blocks on the same columns by a second kernel, from the context's scratch: both in a fixed order. (In
-// clusters the blocks do not fill the device: 96 of 148 multiprocessors for 16 tiles of columns.)
+// and so are the blocks on the same columns, both in a fixed order: through a cluster's shared memory, or, as clusters do not
+// fill the device, by a second kernel from the context's scratch. That takes 4 us, a cluster's barriers one.
 constexpr float UP = 0x1p110f, BACK = 0x1p23f;             // 2^110 2^-133 2^23 = 1
 constexpr int G_ROWS = 32;                                 // of a stage
 constexpr int G_CODES = G_ROWS * COLS / 2;                 // bytes
@@ -486,26 +493,29 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
     const uint32_t put_d = ring + G_CODES + n_at * (PIECES * 16) + ((c_at ^ (F32 ? (n_at & 1) << 2 : (n_at >> 1 & 1) << 1)) << 4);
     const char *d_at = (const char *)A.in + ((int64_t)(n0 + n_at) * A.in_stride + slab * G_ROWS + c_at * (16 / ESZ)) * ESZ;
     const int64_t d_step = (int64_t)slabs * G_ROWS * ESZ, d_token = 32 / PIECES * A.in_stride * ESZ;
+    const int whole = V / G_ROWS;                          // stages of no row behind the last
+    int size[ITEMS];                                       // (nothing is read of a token that there is not: zeros)
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) size[i] = n0 + n_at + i * (32 / PIECES) < A.N ? 16 : 0;
     auto fetch = [&]() {
         if (fs < steps) {
-            const uint32_t to = put + slot_f;
-            if (t < here) {                                // (rows 8 on: the piece's place has another bit)
-                if (fs * G_ROWS + G_ROWS <= V) {
+            const uint32_t to = put + slot_f, to_d = put_d + slot_f;
+            if (fs < whole) {
+                if (t < here) {                            // (rows 8 on: the piece's place has another bit)
                     cp16(to, code_at);
                     cp16((to + 8 * 64) ^ 32, code_at + eight);
                     cp16(to + 16 * 64, code_at + 2 * eight);
                     cp16((to + 24 * 64) ^ 32, code_at + 3 * eight);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        cp16((to + i * 8 * 64) ^ (i & 1 ? 32 : 0), from + (size_t)min(fs * G_ROWS + (lane >> 2) + 8 * i, V - 1) * row_bytes);
                 }
-            }
-            const int bytes = max(0, min(16 / ESZ, V - (fs * G_ROWS + c_at * (16 / ESZ)))) * ESZ;
 #pragma unroll
-            for (int i = 0; i < ITEMS; ++i) {
-                const bool in = bytes > 0 && n0 + n_at + i * (32 / PIECES) < A.N;
-                cp16_part(put_d + slot_f + i * 512, in ? d_at + i * d_token : A.in, in ? bytes : 0);
+                for (int i = 0; i < ITEMS; ++i) cp16_part(to_d + i * 512, size[i] ? d_at + i * d_token : A.in, size[i]);
+            } else {
+                const int bytes = max(0, min(16 / ESZ, V - (fs * G_ROWS + c_at * (16 / ESZ)))) * ESZ;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (t < here) cp16((to + i * 8 * 64) ^ (i & 1 ? 32 : 0), from + (size_t)min(fs * G_ROWS + (lane >> 2) + 8 * i, V - 1) * row_bytes);
+#pragma unroll
+                for (int i = 0; i < ITEMS; ++i) cp16_part(to_d + i * 512, size[i] && bytes ? d_at + i * d_token : A.in, min(size[i], bytes));
             }
             fs += slabs;
             code_at += code_step;
@@ -631,7 +641,8 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
                                 f2_unpack(rest, lo, hi);
                                 b[half][q][k][p] = halves(__float_as_uint(lo), __float_as_uint(hi), HIGH);
                                 if (p + 1 < P)
-                                    rest = f2_add(rest, f2_pack(-__uint_as_float(__float_as_uint(lo) & 0xFFFF0000u), -__uint_as_float(__float_as_uint(hi) & 0xFFFF0000u)));
+                                    rest = f2_fma(f2_pack(__uint_as_float(__float_as_uint(lo) & 0xFFFF0000u), __uint_as_float(__float_as_uint(hi) & 0xFFFF0000u)),
+                                                  f2_pack(-1.f, -1.f), rest);
                             }
                         }
                 // four codes of a lane in each of four rows: two columns of two sums
@@ -695,9 +706,22 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
         float v = part[i];
         for (int w = cw; w < WARPS; w += cw) v += part[w * PART + i];
         const int n = n0 + i % PART / COLS, h = (tile * cw + i / PART) * COLS + i % COLS;
-        if (split > 1) A.parts[(size_t)blockIdx.x * (cw * PART) + i] = v;
+        if (A.cluster) part[i] = v;
+        else if (split > 1) A.parts[(size_t)blockIdx.x * (cw * PART) + i] = v;
         else if (n < A.N && h < H) store(A, n, h, v);
     }
+    if (!A.cluster) return;
+    __syncthreads();
+    od_cluster_arrive(); od_cluster_wait();
+    // each block has a share of the cluster's columns
+    for (int i = cw * PART * rank / split + threadIdx.x; i < cw * PART * (rank + 1) / split; i += THREADS) {
+        const int n = n0 + i % PART / COLS, h = (tile * cw + i / PART) * COLS + i % COLS;
+        float v = 0.f;
+#pragma unroll 4
+        for (int r = 0; r < split; ++r) v += load_cluster(part + i, r);
+        if (n < A.N && h < H) store(A, n, h, v);
+    }
+    od_cluster_arrive(); od_cluster_wait();                // (nobody leaves while another reads)
 }
 
 // The blocks on the same columns: [tile][split][warp side by side][token][column]. A block of threads has 32 numbers,
@@ -762,21 +786,24 @@ Variant variant(bool backward, int32_t G, bool f32, int N, int32_t H)
 }
 
 template <typename K, typename... A>
-cudaError_t launch(K kernel, dim3 grid, dim3 threads, int smem, bool pdl, cudaStream_t s, A... args)
+cudaError_t launch(K kernel, dim3 grid, dim3 threads, int smem, int cluster, bool pdl, cudaStream_t s, A... args)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid; cfg.blockDim = threads;
     cfg.dynamicSmemBytes = smem; cfg.stream = s;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr; cfg.numAttrs = pdl ? 1 : 0;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)cluster; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr; cfg.numAttrs = pdl ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 }  // namespace
 
-cudaError_t od_q4_prepare_device()
+// the kernels' limits; clusters[n]: clusters of n blocks of the gradient that are resident at a time
+cudaError_t od_q4_prepare_device(int32_t *clusters)
 {
     Kernel done = nullptr;
     // (every variant: these sizes reach one, two, four parts of 8 tokens, rings of three and two stages, and none in shared memory)
@@ -787,10 +814,26 @@ cudaError_t od_q4_prepare_device()
                     for (int32_t H = 128; H <= 65536; H += H < 16384 ? 128 : 49152) {
                         const Variant v = variant(backward, G, f32, N, H);
                         if (v.kernel == done) continue;
-                        const cudaError_t e = cudaFuncSetAttribute((const void *)v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST);
+                        cudaError_t e = cudaFuncSetAttribute((const void *)v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST);
+                        if (e == cudaSuccess && backward) e = cudaFuncSetAttribute((const void *)v.kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
                         if (e != cudaSuccess) return e;
                         done = v.kernel;
                     }
+    for (int n = 0; n <= OD_Q4_MAX_SPLIT; ++n) {           // (the variant with the most shared memory; each fills a multiprocessor)
+        const Variant v = variant(true, 32, true, 16, 128);
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)n; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.gridDim = dim3((unsigned)n); cfg.blockDim = dim3(v.threads); cfg.dynamicSmemBytes = v.smem;
+        cfg.attrs = attr; cfg.numAttrs = 1;
+        int here = 0;
+        if (n < 2 || cudaOccupancyMaxActiveClusters(&here, (const void *)v.kernel, &cfg) != cudaSuccess) {
+            cudaGetLastError();
+            here = 0;
+        }
+        clusters[n] = here;
+    }
     return cudaSuccess;
 }
 
@@ -800,7 +843,7 @@ cudaError_t od_launch_q4(const od_ctx *c, bool backward, int32_t N, int32_t V, i
     const bool f32 = a_dtype == OD_F32, pdl = c->opt_pdl != 0;
     const int32_t sms = c->sm_count;
     Q4Args args = {a, as, (const uint8_t *)codes, (const unsigned short *)scales, b, bs, N, V, H, f32, b_dtype == OD_F32,
-                   H % COLS == 0 && ((uintptr_t)scales & 7u) == 0, 1, 1, 1, 0, c->d_q4_parts};
+                   H % COLS == 0 && ((uintptr_t)scales & 7u) == 0, 1, 1, 1, 0, 0, c->d_q4_parts};
     if (!backward) {
         const Variant v = variant(false, G, f32, N, H);
         const int64_t units = ((int64_t)V + ROWS - 1) / ROWS, blocks = units < sms ? units : sms;
@@ -811,26 +854,34 @@ cudaError_t od_launch_q4(const od_ctx *c, bool backward, int32_t N, int32_t V, i
             const int64_t cost = (each * ks + F_WARPS - 1) / F_WARPS * ((stages + ks - 1) / ks);
             if (cost < best) { best = cost; args.k_split = ks; }
         }
-        return launch(v.kernel, dim3((unsigned)blocks, (unsigned)((N + v.tokens - 1) / v.tokens)), F_THREADS, v.smem, pdl, s, args);
+        return launch(v.kernel, dim3((unsigned)blocks, (unsigned)((N + v.tokens - 1) / v.tokens)), F_THREADS, v.smem, 1, pdl, s, args);
     }
     // 16 tokens at a time, then 8: the scratch is for one time
     for (int32_t n = 0; n < N;) {
         const Variant v = variant(true, G, f32, N - n, H);
-        // Warps side by side (4, 2, 1) and blocks on the same columns (as many as there are multiprocessors for): the fewest
-        // stages of a warp; of equal ones the widest rows.
-        const int64_t steps = ((int64_t)V + G_ROWS - 1) / G_ROWS;
+        // Warps side by side (4, 2, 1), blocks on the same columns (as many as there are multiprocessors for, or a cluster of
+        // any size) and how these are joined, by the time that it takes in twentieths of a us, as measured: a stage of a warp 13, and
+        // for every eight tokens 13, 6 for each group of its columns but one and 6 if they are fp32; the join 80, a cluster 20.
+        // Of equal ones the widest rows.
+        const int64_t steps = ((int64_t)V + G_ROWS - 1) / G_ROWS, stage = 13 + v.tokens / 8 * (13 + 6 * (128 / G - 1) + 6 * f32);
         int64_t best = INT64_MAX, blocks = 0;
+        auto offer = [&](int32_t cw, int64_t split, int64_t rounds, int64_t join, bool cluster) {
+            const int64_t slabs = split * (WARPS / cw), cost = rounds * ((steps + slabs - 1) / slabs) * stage + join;
+            if (cost >= best) return;
+            best = cost; blocks = (H + cw * COLS - 1) / (cw * COLS) * split;
+            args.col_warps = cw; args.split = (int32_t)split; args.cluster = cluster;
+        };
         for (int32_t cw = 4 * 8 / v.tokens; cw >= 1; cw /= 2) {
-            const int64_t tiles = (H + cw * COLS - 1) / (cw * COLS), deep = WARPS / cw;
-            int64_t split = sms / tiles < 1 ? 1 : sms / tiles;
-            if (split > (steps + deep - 1) / deep) split = (steps + deep - 1) / deep;
-            const int64_t cost = (tiles * split + sms - 1) / sms * ((steps + split * deep - 1) / (split * deep));
-            if (cost < best) { best = cost; blocks = tiles * split; args.col_warps = cw; args.split = (int32_t)split; }
+            const int64_t tiles = (H + cw * COLS - 1) / (cw * COLS), deep = WARPS / cw, most = (steps + deep - 1) / deep;
+            const int64_t split = tiles > sms ? 1 : sms / tiles < most ? sms / tiles : most;
+            offer(cw, split, (tiles * split + sms - 1) / sms, split > 1 ? 80 : 0, false);
+            for (int32_t k = 2; k <= OD_Q4_MAX_SPLIT && k <= most; ++k)
+                if (c->q4_clusters[k] > 0) offer(cw, k, (tiles + c->q4_clusters[k] - 1) / c->q4_clusters[k], 20, true);
         }
         args.first_token = n;
-        cudaError_t e = launch(v.kernel, dim3((unsigned)blocks), THREADS, v.smem, pdl, s, args);
-        if (e == cudaSuccess && args.split > 1)
-            e = launch(od_q4_join_kernel, dim3((unsigned)(H / 32), (unsigned)(N - n < v.tokens ? N - n : v.tokens)), dim3(32, JOIN), 0, pdl, s, args, v.tokens);
+        cudaError_t e = launch(v.kernel, dim3((unsigned)blocks), THREADS, v.smem, args.cluster ? args.split : 1, pdl, s, args);
+        if (e == cudaSuccess && args.split > 1 && !args.cluster)
+            e = launch(od_q4_join_kernel, dim3((unsigned)(H / 32), (unsigned)(N - n < v.tokens ? N - n : v.tokens)), dim3(32, JOIN), 0, 1, pdl, s, args, v.tokens);
         if (e != cudaSuccess) return e;
         n += v.tokens;
     }

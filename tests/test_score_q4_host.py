@@ -130,9 +130,29 @@ def test_launches_of_the_layer(lib):
     assert [x[1:] for x in launches(N=33, V=32000, H=1024)] == [(148, 2)]
     assert [x[1:] for x in launches(N=33, V=32000, H=4096)] == [(148, 3)]              # 16 tokens fit
     assert [x[1:] for x in launches(N=33, V=32000, H=65536)] == [(148, 5)]             # (none do: 8 at a time)
-    # backward: 16 tokens at a time and what is left, each with a join where blocks share columns
-    got = launches(N=24, V=32000, H=2048, backward=True)
-    assert len(got) == 4 and all(b <= 148 for _, b, _ in got[0::2]) and [x[2] for x in got[1::2]] == [16, 8]
-    assert got[1][1] == got[3][1] == 2048 // 32
+    # backward: one launch of clusters for a short layer
+    (_, blocks, y), = launches(N=8, V=32000, H=768, backward=True)
+    assert blocks <= 148 and y == 1
     assert len(launches(N=8, V=16, H=2048, backward=True)) == 1                         # nothing to join
     assert len(launches(N=1, V=304, H=65536, backward=True)) == 1                       # more columns than multiprocessors
+
+
+@pytest.fixture
+def without_clusters():
+    """A device with no room for clusters of the gradient's blocks."""
+    L = helpers.fake_runtime_lib()
+    L.fake_no_driver_functions(1)                           # (what is known of the device is not kept then)
+    L.fake_cluster_limit(1)
+    yield
+    L.fake_cluster_limit(16)
+    L.fake_no_driver_functions(0)
+
+
+def test_the_gradients_join(without_clusters):
+    """Where blocks that are no cluster share columns a second kernel joins them, 16 tokens at a time and what is left."""
+    lib = Lib()
+    assert lib.q4(N=24, V=32000, H=2048, backward=True) == OK
+    got = lib.log()
+    assert len(got) == 4 and all(b <= 148 and y == 1 for _, b, y in got[0::2])
+    assert [x[1:] for x in got[1::2]] == [(2048 // 32, 16), (2048 // 32, 8)]
+    lib.close()
