@@ -133,7 +133,7 @@ enum od_counter {
 #define OD_TAU_EXIT 4.0e-6f
 
 /* flags[b,r] written by od_token_logprobs */
-#define OD_LF_BAD_TEMPERATURE 0x1u /* not positive and finite: nothing of the row was read */
+#define OD_LF_BAD_TEMPERATURE 0x1u /* not positive and finite (or its reciprocal not) */
 #define OD_LF_NONFINITE 0x2u       /* the row holds NaN or +inf: its results are NaN */
 #define OD_LF_NO_MASS 0x4u         /* every logit of the row is -inf */
 #define OD_LF_BAD_ID 0x8u          /* the given id is outside the vocabulary and not -1 */

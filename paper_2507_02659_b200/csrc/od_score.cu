@@ -237,13 +237,39 @@ __global__ void __launch_bounds__(THREADS, 4) od_score_kernel(const ScoreArgs A)
     const uint32_t split = A.split, part = blockIdx.x % split;
     const int64_t r = blockIdx.x / split;
     const int32_t b = (int32_t)(r / A.R), rr = (int32_t)(r % A.R);
-    // (the blocks of a cluster leave together)
-    if (A.n_rows && rr >= A.n_rows[b]) return;
+    // (asked for at once; the blocks of a cluster leave together)
+    const int live = A.n_rows ? A.n_rows[b] : A.R;
     const float T = A.temperature ? A.temperature[b] : 1.f;
+    const int id = A.ids ? A.ids[r] : -1;
+    if (rr >= live) return;
     const char *row = A.logits + b * A.seq_bytes + rr * A.row_bytes;
     const int V = A.V, n = A.n_top;
-    const int id = A.ids ? A.ids[r] : -1;
     const uint32_t bad_id = id < -1 || id >= V ? OD_LF_BAD_ID : 0u;
+    // the slice of this block, by vectors
+    const int nvec = (V - 1) / VEC<DTYPE> + 1;
+    const int lo = (int)((int64_t)nvec * part / split), hi = (int)((int64_t)nvec * (part + 1) / split);
+    const uint4 none = make_uint4(NONE<DTYPE>, NONE<DTYPE>, NONE<DTYPE>, NONE<DTYPE>);
+    // turns of the loop to a slot: 2^per
+    const int turns = (hi - lo + U * THREADS - 1) / (U * THREADS);
+    int per = 0;
+    while (turns > SLOTS << per) ++per;
+    Sums t = {-FLT_MAX, 0.f, 0.f};
+    uint4 x[U], y[U];
+    // turns whose loads are all whole vectors of this block's slice
+    const int whole = max(0, min(hi, V / VEC<DTYPE>) - lo) / (U * THREADS);
+    const char *next = row + (size_t)(lo + tid) * 16;
+    auto load = [&](uint4 (&v)[U], int turn) {
+        if (turn < whole) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = ld_stream(next + u * THREADS * 16);
+            next += U * THREADS * 16;
+        } else {
+            const int i = lo + tid + turn * (U * THREADS);
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = i + u * THREADS < hi ? load_vec<DTYPE>(row, i + u * THREADS, V) : none;
+        }
+    };
+    load(x, 0);
     if (!usable(T)) {
         if (part == 0) {
             if (tid == 0) {
@@ -265,48 +291,20 @@ __global__ void __launch_bounds__(THREADS, 4) od_score_kernel(const ScoreArgs A)
     float x_t = 0.f;                                       // requested early, by the thread that uses it
     if (tid == 0 && part == 0 && id >= 0 && id < V) x_t = od_load_logit<DTYPE>(row, id);
 
-    // the slice of this block, by vectors
-    const int nvec = (V - 1) / VEC<DTYPE> + 1;
-    const int lo = (int)((int64_t)nvec * part / split), hi = (int)((int64_t)nvec * (part + 1) / split);
-    const uint4 none = make_uint4(NONE<DTYPE>, NONE<DTYPE>, NONE<DTYPE>, NONE<DTYPE>);
-    // turns of the loop to a slot: 2^per
-    const int turns = (hi - lo + U * THREADS - 1) / (U * THREADS);
-    int per = 0;
-    while (turns > SLOTS << per) ++per;
-    Sums t = {-FLT_MAX, 0.f, 0.f};
-    uint4 x[U];
-    {
-        uint4 y[U];
-        // turns whose loads are all whole vectors of this block's slice
-        const int whole = max(0, min(hi, V / VEC<DTYPE>) - lo) / (U * THREADS);
-        const char *next = row + (size_t)(lo + tid) * 16;
-        auto load = [&](uint4 (&v)[U], int turn) {
-            if (turn < whole) {
-#pragma unroll
-                for (int u = 0; u < U; ++u) v[u] = ld_stream(next + u * THREADS * 16);
-                next += U * THREADS * 16;
-            } else {
-                const int i = lo + tid + turn * (U * THREADS);
-#pragma unroll
-                for (int u = 0; u < U; ++u) v[u] = i + u * THREADS < hi ? load_vec<DTYPE>(row, i + u * THREADS, V) : none;
-            }
-        };
-        auto take = [&](const uint4 (&v)[U], int turn) {
-            float m = absorb<DTYPE>(t, v, scale);
-            if (TOP) {
-                float &most = maxima[turn >> per][tid];
-                if (turn & (1 << per) - 1) m = fmaxf(m, most);
-                most = m;
-            }
-        };
-        load(x, 0);
-        for (int k = 0; k < turns; k += 2) {
-            if (k + 1 < turns) load(y, k + 1);
-            take(x, k);
-            if (k + 1 == turns) break;
-            if (k + 2 < turns) load(x, k + 2);
-            take(y, k + 1);
+    auto take = [&](const uint4 (&v)[U], int turn) {
+        float m = absorb<DTYPE>(t, v, scale);
+        if (TOP) {
+            float &most = maxima[turn >> per][tid];
+            if (turn & (1 << per) - 1) m = fmaxf(m, most);
+            most = m;
         }
+    };
+    for (int k = 0; k < turns; k += 2) {
+        if (k + 1 < turns) load(y, k + 1);
+        take(x, k);
+        if (k + 1 == turns) break;
+        if (k + 2 < turns) load(x, k + 2);
+        take(y, k + 1);
     }
     if (TOP) {
         float g = t.c;
@@ -533,14 +531,18 @@ __global__ void __launch_bounds__(THREADS) od_score_grad_kernel(const ScoreGradA
     const char *row = A.logits + b * A.seq_bytes + rr * A.row_bytes;
     char *out = A.grad + b * A.grad_seq_bytes + rr * A.grad_row_bytes;
     const int nvec = (V - 1) / VEC<DTYPE> + 1, per_block = A.turns * (U * THREADS), lo = chunk * per_block, hi = min(nvec, lo + per_block);
-    const bool counts = !A.n_rows || rr < A.n_rows[b];
-    const float T = A.temperature ? A.temperature[b] : 1.f;
-    const float S = counts ? A.row_sum[r] : 0.f;
-    if (!counts || !usable(T) || S == 0.f) {
+    // (all that is asked for at once: none of it hangs on another)
+    const int live = A.n_rows ? A.n_rows[b] : A.R;
+    const float T = A.temperature ? A.temperature[b] : 1.f, S = A.row_sum[r], M = A.row_max[r];
+    const float g_h = ENTROPY ? A.g_entropy[r] : 0.f, H = ENTROPY ? A.entropy[r] : 0.f;
+    int id = A.ids && A.g_logprob ? A.ids[r] : -1, top = -1;
+    float g_id = A.ids && A.g_logprob ? A.g_logprob[r] : 0.f, g = 0.f;
+    if (A.g_top && lane < n) { top = A.top_ids[r * n + lane]; g = A.g_top[r * n + lane]; }
+    auto zeros = [&]() {
         const float zero[VEC<DTYPE>] = {};
         for (int i = lo + tid; i < hi; i += THREADS) store_vec<DTYPE>(out, i, V, zero);
-        return;
-    }
+    };
+    if (rr >= live) { zeros(); return; }
     const int whole = max(0, min(hi, V / VEC<DTYPE>) - lo) / (U * THREADS), turns = (hi - lo + U * THREADS - 1) / (U * THREADS);
     auto load = [&](uint4 (&v)[U], int turn) {
         const int i = lo + turn * (U * THREADS) + tid;
@@ -555,36 +557,32 @@ __global__ void __launch_bounds__(THREADS) od_score_grad_kernel(const ScoreGradA
     };
     uint4 x[U], y[U];
     load(x, 0);
+    if (!usable(T) || S == 0.f) { zeros(); return; }
 
     // every warp sums the weights itself, in the same order
-    const float M = A.row_max[r], ln_s = logf(S), scale = LOG2E / T;
-    const int id = A.ids && A.g_logprob ? A.ids[r] : -1;
-    const bool given = id >= 0 && id < V;
-    const float g_id = given ? A.g_logprob[r] : 0.f;
-    int top = -1;
-    float g = 0.f;
-    if (A.g_top && lane < n) top = A.top_ids[r * n + lane];
-    if (top >= V) top = -1;
-    if (top >= 0) g = A.g_top[r * n + lane];
+    const float ln_s = logf(S), scale = LOG2E / T;
+    if (id < 0 || id >= V) { id = -1; g_id = 0.f; }
+    if (top < 0 || top >= V) { top = -1; g = 0.f; }
     float G = g;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) G += __shfl_xor_sync(0xFFFFFFFFu, G, o);
     G += g_id;
-    if (tid < 32) { given_id[lane] = top; given_g[lane] = g; }
-    if (tid == 0) { given_id[OD_MAX_TOP] = given ? id : -1; given_g[OD_MAX_TOP] = g_id; }
+    // the alternatives and behind them the given id
+    if (tid < n) { given_id[tid] = top; given_g[tid] = g; }
+    if (tid == 0) { given_id[n] = id; given_g[n] = g_id; }
     __syncthreads();
-    const float g_h = ENTROPY ? A.g_entropy[r] : 0.f, per = -1.f / (S * T);
-    const float c0 = per * (G + (ENTROPY ? g_h * (A.entropy[r] - ln_s) : 0.f)), c1 = per * g_h * LN2;
+    const float per = -1.f / (S * T);
+    const float c0 = per * (G + (ENTROPY ? g_h * (H - ln_s) : 0.f)), c1 = per * g_h * LN2;
 
     // the value of a given id in this chunk: it is written by the first entry that names it, with the sum of their weights
     int write = -1;
     float value = 0.f;
-    if (tid < GIVEN) {
+    if (tid <= n) {
         const int j = given_id[tid], i = j / VEC<DTYPE>;
         if (j >= 0 && i >= lo && i < hi) {
             float sum = 0.f;
             bool first = true;
-            for (int k = 0; k < GIVEN; ++k)
+            for (int k = 0; k <= n; ++k)
                 if (given_id[k] == j) { sum += given_g[k]; first = first && k >= tid; }
             if (first) {
                 const float xj = DTYPE == OD_F32 ? __ldcs((const float *)row + j) : __uint_as_float((uint32_t)__ldcs((const unsigned short *)row + j) << 16);
