@@ -458,9 +458,8 @@ int32_t od_token_logprobs_grad(od_ctx *ctx, int32_t B, int32_t R, int32_t vocab,
  *   logits[n,v] = sum_h hidden[n,h] w[v,h],   g_hidden[n,h] = sum_v g_logits[n,v] w[v,h].
  * Sums are fp32, nothing is rounded before them: a product of an input and a code is exact, scales
  * are applied to sums over a group (logits) or to the input (gradient, one fp32 rounding). Infinities
- * and NaN of the inputs give what the formula gives; scales are finite. (Digits go lost, as in fp32's
- * smallest numbers, of hidden states below 2^-90 of their token's largest and of gradient times scale
- * below 2^-103.)
+ * and NaN of the inputs give what the formula gives; scales are finite. (Hidden states below 2^-90 of
+ * their token's largest lose digits, as fp32's smallest numbers do.)
  *   in  (device) hidden / g_logits fp32 or bf16, N rows, row stride in elements, base and stride
  *                multiples of 16 bytes
  *                codes  uint8[vocab, hidden_size / 2], dense, 16-byte aligned: column 2i of a row in

@@ -8,13 +8,13 @@
 // of fp32 sums (and of an fp32 gradient times its scale). The scale of a group belongs to a row of the weights: forward
 // it multiplies the group's sum, backward, where rows are summed over, the gradient.
 //
-// For a few tokens the codes are all there is to move, and unpacking them is what competes with that. Nothing is subtracted
-// from a code and nothing or'ed to it: with no more than eight bits set a bf16 number is its bits times 2^-133 (in the first
-// binade too), so two masks, a shift and two masks make eight codes u, half of them as 16 u, ready for the tensor pipe. The
-// inputs are scaled by a power of two so that products are in fp32's range, and where a 16 u meets an input that one is
-// divided by 16 (forward) or the result is (backward). The 8 is taken off in sums: of a group's inputs (forward, where the
-// group's sum begins), of all scaled gradients (backward, at the end). It adds no more to the sums' magnitudes than the
-// codes do. (Eight tokens through 128256 x 4096: 59 us with 136 subtracted from bf16 numbers 128 + u, 52 us so.)
+// For a few tokens the codes are all there is to move, and unpacking them is what competes with that. Forward nothing is
+// subtracted from a code and nothing or'ed to it: with no more than eight bits set a bf16 number is its bits times 2^-133 (in
+// the first binade too), so two masks, a shift and two masks make eight codes u, half of them as 16 u, ready for the tensor
+// pipe. The inputs are scaled by a power of two so that products are in fp32's range, and divided by 16 where they meet a
+// 16 u. The 8 is taken off in what a group's sum begins at, -8 times the sum of its inputs, which adds no more to the sum's
+// magnitudes than the codes do. (Eight tokens through 128256 x 4096: 59 us with 136 subtracted from bf16 numbers 128 + u,
+// 52 us so.)
 // Operands go from registers into mma.sync: for tcgen05 they would be written to shared memory and read there at two
 // bytes a weight, 29 us of its bandwidth for 128256 x 2048, whose codes HBM brings in 21.
 //
@@ -48,6 +48,7 @@ struct Q4Args {
     int64_t out_stride;
     int32_t N, V, H, in_f32, out_f32;
     int32_t wide_scales;                                   // the scales of a stage's row are one aligned word
+    uint32_t bf16_128;                                     // see unpack
     int32_t k_split;                                       // forward: warps to the same rows
     int32_t split, col_warps;                              // backward: blocks on the same columns, warps side by side
     int32_t cluster;                                       // the blocks on the same columns are one
@@ -81,12 +82,6 @@ __device__ __forceinline__ float load_cluster(const float *p, uint32_t rank)
     asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(od_cluster_address(p, rank)) : "memory");
     return v;
 }
-__device__ __forceinline__ float max_nan(float a, float b)
-{
-    float d;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
-    return d;
-}
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -98,6 +93,17 @@ __device__ __forceinline__ uint32_t halves(uint32_t a, uint32_t b, uint32_t pick
     return __byte_perm(a, b, pick);
 }
 constexpr uint32_t CODE = 0x000F000Fu, CODE16 = 0x00F000F0u;
+// Codes I and I + 4 of a word, less 8, as a pair of bf16: 128 + u has u in its last bits. (bf16_128, a pair of 128, is an
+// argument of the kernel: a mask and an or with two constants that the compiler knows are two instructions, with one in a
+// register they are one.)
+template <int I>
+__device__ __forceinline__ uint32_t unpack(uint32_t w, uint32_t bf16_128)
+{
+    uint32_t m, d;
+    asm("lop3.b32 %0, %1, 0x000F000F, %2, 0xEA;" : "=r"(m) : "r"(w >> 4 * I), "r"(bf16_128));
+    asm("sub.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(m), "r"(0x43084308u));
+    return d;
+}
 constexpr uint32_t LOW = 0x5410, HIGH = 0x7632;            // both low halves, both high halves
 
 // P pieces of a pair as bf16 pairs: the leading 8 bits of what is left, which are cut off it
@@ -445,13 +451,14 @@ __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
 // ---- backward: 128 columns to a warp, every so many-th 32 rows ----------------------------------
 //
 // Rows are summed over: two of them are the pair of an operand, four columns in a row are a half word. The tokens' side is
-// made anew for each group: gradient times scale, in pieces. It is scaled by 2^110 for what the codes are as bf16 numbers;
-// what is too large for that (and infinities and NaN) is added to the sums on its own. The 8 of a code is taken off at the
-// end: sums of gradient times scale, of which a lane has those of its rows.
+// made anew for each group: gradient times scale, in pieces. The codes are brought to u - 8 here, as ordinary bf16 numbers
+// (two shifts or masks more and a subtraction for two codes, 5 % of the time). Gradients have mostly one sign (a softmax but
+// for one large entry), and where sums of them with 0 to 15 were taken the tensor pipe's cuts were 1e-5 of the result; with
+// numbers below bf16's normal ones, which the pipe lines up as if their leading bits were there, 1e-6; so they are 4e-7,
+// as plain fp32 sums' are.
 // Warps side by side share rows (a block reads up to 256 bytes in a row). Those on the same columns are summed at the end,
 // and so are the blocks on the same columns, both in a fixed order: through a cluster's shared memory, or, as clusters do not
 // fill the device, by a second kernel from the context's scratch. That takes 4 us, a cluster's barriers one.
-constexpr float UP = 0x1p110f, BACK = 0x1p23f;             // 2^110 2^-133 2^23 = 1
 constexpr int G_ROWS = 32;                                 // of a stage
 constexpr int G_CODES = G_ROWS * COLS / 2;                 // bytes
 
@@ -540,12 +547,11 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
     const uint32_t get = ring + 4 * t * 64 + (PAIRS ? g & 3 : g >> 1) * 4, pick = g & 1 ? HIGH : LOW;
     const uint32_t get_d = ring + G_CODES + g * (PIECES * 16) + (F32 ? (t ^ (g & 1) << 2) << 4 : (g >> 1 & 1) << 5 | t << 3);
     float acc[8][NT][4] = {};
-    uint64_t eights[GROUPS][NT] = {};                      // pairs of sums
     int slot = 0, flip = 0;
     if (slab < steps) load_scales(slab);
     for (int s = slab; s < steps; s += slabs) {
 #pragma unroll
-        for (int i = 0; i < GROUPS; ++i) scale_of[(flip * G_ROWS + lane) * GROUPS + i] = raw.get(i) * UP;
+        for (int i = 0; i < GROUPS; ++i) scale_of[(flip * G_ROWS + lane) * GROUPS + i] = raw.get(i);
         if (s + slabs < steps) load_scales(s + slabs);
         cp_wait<G_RING - 2>();
         __syncwarp();
@@ -591,41 +597,9 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
                             z[half][q][k] = f2_mul(f2_pack(d[half][q][2 * k], d[half][q][2 * k + 1]), f2_pack(e[half][2 * k][i], e[half][2 * k + 1][i]));
                             float lo, hi;
                             f2_unpack(z[half][q][k], lo, hi);
-                            m = max_nan(max_nan(m, fabsf(lo)), fabsf(hi));
+                            m = fmaxf(fmaxf(m, fabsf(lo)), fabsf(hi));
                         }
-                if (__any_sync(0xFFFFFFFFu, !(m < INFINITY))) {
-                    // too large to be scaled, infinite or NaN (or nothing, and the scale too large)
-#pragma unroll
-                    for (int half = 0; half < SIDE; ++half)
-#pragma unroll
-                        for (int q = 0; q < NT; ++q)
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                float lo, hi;
-                                f2_unpack(z[half][q][k / 2], lo, hi);
-                                const bool large = !(fabsf(k & 1 ? hi : lo) < INFINITY);
-                                float big = 0.f;
-                                if (large) {
-                                    const int v = s * G_ROWS + (base + half) * 16 + 4 * t + k;      // (behind the last row the scale is zero)
-                                    big = d[half][q][k] * (1.f / BACK) * __uint_as_float((uint32_t)A.scales[(size_t)v * n_groups + col / (32 * GB) + i] << 16);
-                                    z[half][q][k / 2] = k & 1 ? f2_pack(lo, 0.f) : f2_pack(0.f, hi);
-                                }
-                                for (unsigned lanes = __ballot_sync(0xFFFFFFFFu, large); lanes; lanes &= lanes - 1) {
-                                    const int src = __ffs(lanes) - 1, n = src >> 2, r = (base + half) * 16 + 4 * (src & 3) + k;
-                                    const float f = __shfl_sync(0xFFFFFFFFu, big, src);
-                                    const unsigned char *const row = smem + warp * g_warp<P, NT, GB> + slot + r * 64;
-#pragma unroll
-                                    for (int c = 2 * i * GB; c < 2 * (i + 1) * GB; ++c) {
-                                        // the byte of a lane's two columns of sum c
-                                        const int at = PAIRS ? c / 4 * 32 + 4 * g + c % 4 : c / 2 * 16 + 2 * g + c % 2;
-                                        const uint32_t byte = row[((at >> 4 ^ (r >> 2 & 3)) << 4) + (at & 15)];
-                                        const float lo = f * (float)((int)(byte & 15) - 8), hi = f * (float)((int)(byte >> 4) - 8) * 16.f;
-                                        if (2 * t == n) { acc[c][q][0] += lo; acc[c][q][2] += hi; }
-                                        if (2 * t + 1 == n) { acc[c][q][1] += lo; acc[c][q][3] += hi; }
-                                    }
-                                }
-                            }
-                }
+                const bool guard = __any_sync(0xFFFFFFFFu, m == INFINITY);
                 uint32_t b[SIDE][NT][2][P];
 #pragma unroll
                 for (int half = 0; half < SIDE; ++half)
@@ -633,7 +607,6 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
                     for (int q = 0; q < NT; ++q)
 #pragma unroll
                         for (int k = 0; k < 2; ++k) {
-                            eights[i][q] = f2_fma(z[half][q][k], f2_pack(0x1p-126f * 0.0625f, 0x1p-126f * 0.0625f), eights[i][q]);      // 8 times 2^-133
                             uint64_t rest = z[half][q][k];
 #pragma unroll
                             for (int p = 0; p < P; ++p) {
@@ -643,13 +616,18 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
                                 if (p + 1 < P)
                                     rest = f2_fma(f2_pack(__uint_as_float(__float_as_uint(lo) & 0xFFFF0000u), __uint_as_float(__float_as_uint(hi) & 0xFFFF0000u)),
                                                   f2_pack(-1.f, -1.f), rest);
+                                if (p + 1 < P && guard) {  // (all of an infinity is in its first piece)
+                                    float u, v;
+                                    f2_unpack(rest, u, v);
+                                    rest = f2_pack(fabsf(lo) == INFINITY ? 0.f : u, fabsf(hi) == INFINITY ? 0.f : v);
+                                }
                             }
                         }
                 // four codes of a lane in each of four rows: two columns of two sums
                 auto product = [&](uint32_t w01, uint32_t w23, int half, int c) {
-                    const uint32_t v01 = w01 >> 8, v23 = w23 >> 8;
-                    const uint32_t a0[4] = {w01 & CODE, w01 & CODE16, w23 & CODE, w23 & CODE16};       // (rows 8 on are 16 times as much)
-                    const uint32_t a1[4] = {v01 & CODE, v01 & CODE16, v23 & CODE, v23 & CODE16};
+                    const uint32_t k = A.bf16_128;
+                    const uint32_t a0[4] = {unpack<0>(w01, k), unpack<1>(w01, k), unpack<0>(w23, k), unpack<1>(w23, k)};
+                    const uint32_t a1[4] = {unpack<2>(w01, k), unpack<3>(w01, k), unpack<2>(w23, k), unpack<3>(w23, k)};
 #pragma unroll
                     for (int p = 0; p < P; ++p)
 #pragma unroll
@@ -683,24 +661,14 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
     constexpr int PART = 8 * NT * COLS;                    // numbers of a warp
     float *const part = (float *)smem;
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i)
+    for (int c = 0; c < 8; ++c)
 #pragma unroll
-        for (int q = 0; q < NT; ++q) {
-            float v, more;
-            f2_unpack(eights[i][q], v, more);
-            v += more;
-            v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
-            v += __shfl_xor_sync(0xFFFFFFFFu, v, 2);       // of token g
-            const float e[2] = {__shfl_sync(0xFFFFFFFFu, v, 8 * t), __shfl_sync(0xFFFFFFFFu, v, 8 * t + 4)};
+        for (int q = 0; q < NT; ++q)
 #pragma unroll
-            for (int c = 2 * i * GB; c < 2 * (i + 1) * GB; ++c)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int column = PAIRS ? c / 4 * 64 + 8 * g + c % 4 * 2 : c / 2 * 32 + 4 * g + c % 2 * 2;
-                    *(float2 *)(part + warp * PART + (q * 8 + 2 * t + k) * COLS + column) =
-                        make_float2((acc[c][q][k] - e[k]) * BACK, (acc[c][q][k + 2] * 0.0625f - e[k]) * BACK);
-                }
-        }
+            for (int k = 0; k < 2; ++k) {
+                const int column = PAIRS ? c / 4 * 64 + 8 * g + c % 4 * 2 : c / 2 * 32 + 4 * g + c % 2 * 2;
+                *(float2 *)(part + warp * PART + (q * 8 + 2 * t + k) * COLS + column) = make_float2(acc[c][q][k], acc[c][q][k + 2]);
+            }
     __syncthreads();
     for (int i = threadIdx.x; i < cw * PART; i += THREADS) {
         float v = part[i];
@@ -843,7 +811,7 @@ cudaError_t od_launch_q4(const od_ctx *c, bool backward, int32_t N, int32_t V, i
     const bool f32 = a_dtype == OD_F32, pdl = c->opt_pdl != 0;
     const int32_t sms = c->sm_count;
     Q4Args args = {a, as, (const uint8_t *)codes, (const unsigned short *)scales, b, bs, N, V, H, f32, b_dtype == OD_F32,
-                   H % COLS == 0 && ((uintptr_t)scales & 7u) == 0, 1, 1, 1, 0, 0, c->d_q4_parts};
+                   H % COLS == 0 && ((uintptr_t)scales & 7u) == 0, 0x43004300u, 1, 1, 1, 0, 0, c->d_q4_parts};
     if (!backward) {
         const Variant v = variant(false, G, f32, N, H);
         const int64_t units = ((int64_t)V + ROWS - 1) / ROWS, blocks = units < sms ? units : sms;
