@@ -88,6 +88,12 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void mma_of(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)   // from zero
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
 __device__ __forceinline__ uint32_t halves(uint32_t a, uint32_t b, uint32_t pick)
 {
     return __byte_perm(a, b, pick);
@@ -366,7 +372,8 @@ __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
             cp_wait<RING - 2>();
             __syncwarp();
             fetch();
-            float sum[NT][4];
+            // (of pieces the small ones in a chain of their own: the tensor pipe cuts what it adds to 2^-23 of the largest)
+            float sum[NT][4], small[NT][4];
             auto block = [&](int j) {
                 uint32_t b[NT][P][4];
 #pragma unroll
@@ -385,6 +392,7 @@ __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
                     if (j % GB == 0) {
                         const float2 v = begin_at[(j / GB * NT + q) * 4];
                         sum[q][0] = sum[q][2] = v.x; sum[q][1] = sum[q][3] = v.y;
+                        if (P > 1) small[q][0] = small[q][1] = small[q][2] = small[q][3] = 0.f;
                     }
                 }
                 const uint32_t w0 = lds32((get + slot) ^ (j << 4)), w1 = lds32(((get + slot) ^ (j << 4)) + 8 * 128);
@@ -395,9 +403,12 @@ __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
                 for (int q = 0; q < NT; ++q) {
 #pragma unroll
                     for (int p = 0; p < P; ++p) {
-                        mma(sum[q], a0, b[q][p][0], b[q][p][1]);
-                        mma(sum[q], a1, b[q][p][2], b[q][p][3]);
+                        mma(p == 0 ? sum[q] : small[q], a0, b[q][p][0], b[q][p][1]);
+                        mma(p == 0 ? sum[q] : small[q], a1, b[q][p][2], b[q][p][3]);
                     }
+                    if (P > 1 && j % GB == GB - 1)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) sum[q][k] += small[q][k];
                     if (j % GB == GB - 1) {
                         const float c0 = s0[j / 4].get(j % 4 / GB), c1 = s1[j / 4].get(j % 4 / GB);
                         total[q][0] = fmaf(c0, sum[q][0], total[q][0]); total[q][1] = fmaf(c0, sum[q][1], total[q][1]);
@@ -454,8 +465,8 @@ __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
 // made anew for each group: gradient times scale, in pieces. The codes are brought to u - 8 here, as ordinary bf16 numbers
 // (two shifts or masks more and a subtraction for two codes, 5 % of the time). Gradients have mostly one sign (a softmax but
 // for one large entry), and where sums of them with 0 to 15 were taken the tensor pipe's cuts were 1e-5 of the result; with
-// numbers below bf16's normal ones, which the pipe lines up as if their leading bits were there, 1e-6; so they are 4e-7,
-// as plain fp32 sums' are.
+// numbers below bf16's normal ones, which the pipe lines up as if their leading bits were there, 1e-6; so they are 4e-7, and
+// of fp32 results 2e-7 (EXACT below), where plain fp32 sums are 5e-7 off.
 // Warps side by side share rows (a block reads up to 256 bytes in a row). Those on the same columns are summed at the end,
 // and so are the blocks on the same columns, both in a fixed order: through a cluster's shared memory, or, as clusters do not
 // fill the device, by a second kernel from the context's scratch. That takes 4 us, a cluster's barriers one.
@@ -470,7 +481,10 @@ __device__ __forceinline__ void cp16_part(uint32_t to, const void *from, int byt
 template <int P, int NT> constexpr int g_stage = G_CODES + 8 * NT * G_ROWS * (P == 3 ? 4 : 2);
 template <int P, int NT, int GB> constexpr int g_warp = G_RING * g_stage<P, NT> + 2 * G_ROWS * (4 / GB) * 4;
 
-template <int P, int NT, int GB>
+// EXACT, for fp32 results: the tensor pipe cuts what it adds to its accumulators (to 2^-23 of the largest), so what it adds up in a
+// stage begins at zero and is then added to the sums in fp32 as such, which rounds (128256 x 1824, 28 positions: 2e-6 of the
+// result otherwise, where plain fp32 sums are 7e-7 off).
+template <int P, int NT, int GB, bool EXACT>
 __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
 {
     extern __shared__ __align__(128) unsigned char smem[];
@@ -623,32 +637,49 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
                                 }
                             }
                         }
-                // four codes of a lane in each of four rows: two columns of two sums
-                auto product = [&](uint32_t w01, uint32_t w23, int half, int c) {
+                // four codes of a lane in each of four rows, of both halves: two columns of two sums
+                auto product = [&](const uint32_t (&w01)[SIDE], const uint32_t (&w23)[SIDE], int c) {
                     const uint32_t k = A.bf16_128;
-                    const uint32_t a0[4] = {unpack<0>(w01, k), unpack<1>(w01, k), unpack<0>(w23, k), unpack<1>(w23, k)};
-                    const uint32_t a1[4] = {unpack<2>(w01, k), unpack<3>(w01, k), unpack<2>(w23, k), unpack<3>(w23, k)};
 #pragma unroll
-                    for (int p = 0; p < P; ++p)
+                    for (int upper = 0; upper < 2; ++upper) {
+                        float sum[NT][4];
 #pragma unroll
-                        for (int q = 0; q < NT; ++q) {
-                            mma(acc[c][q], a0, b[half][q][0][p], b[half][q][1][p]);
-                            mma(acc[c + 1][q], a1, b[half][q][0][p], b[half][q][1][p]);
+                        for (int half = 0; half < SIDE; ++half) {
+                            uint32_t a[4];
+                            if (upper) { a[0] = unpack<2>(w01[half], k); a[1] = unpack<3>(w01[half], k); a[2] = unpack<2>(w23[half], k); a[3] = unpack<3>(w23[half], k); }
+                            else { a[0] = unpack<0>(w01[half], k); a[1] = unpack<1>(w01[half], k); a[2] = unpack<0>(w23[half], k); a[3] = unpack<1>(w23[half], k); }
+#pragma unroll
+                            for (int p = 0; p < P; ++p)
+#pragma unroll
+                                for (int q = 0; q < NT; ++q) {
+                                    if (!EXACT) mma(acc[c + upper][q], a, b[half][q][0][p], b[half][q][1][p]);
+                                    else if (half == 0 && p == 0) mma_of(sum[q], a, b[half][q][0][p], b[half][q][1][p]);
+                                    else mma(sum[q], a, b[half][q][0][p], b[half][q][1][p]);
+                                }
                         }
+                        if (EXACT)
+#pragma unroll
+                            for (int q = 0; q < NT; ++q)
+#pragma unroll
+                                for (int e = 0; e < 4; e += 2) {
+                                    float (&to)[4] = acc[c + upper][q];
+                                    f2_unpack(f2_add(f2_pack(to[e], to[e + 1]), f2_pack(sum[q][e], sum[q][e + 1])), to[e], to[e + 1]);
+                                }
+                    }
                 };
 #pragma unroll
-                for (int j = i * GB; j < (i + 1) * GB; j += PAIRS ? 2 : 1)
+                for (int j = i * GB; j < (i + 1) * GB; j += PAIRS ? 2 : 1) {
+                    uint32_t low01[SIDE], low23[SIDE], high01[SIDE], high23[SIDE];
 #pragma unroll
                     for (int half = 0; half < SIDE; ++half) {
                         const uint32_t at = get + slot + (base + half) * 16 * 64 + ((PAIRS ? (j + (g >> 2)) ^ t : j ^ t) << 4);
                         const uint32_t w0 = lds32(at), w1 = lds32(at + 64), w2 = lds32(at + 128), w3 = lds32(at + 192);
-                        if constexpr (PAIRS) {
-                            product(halves(w0, w1, LOW), halves(w2, w3, LOW), half, 2 * j);
-                            product(halves(w0, w1, HIGH), halves(w2, w3, HIGH), half, 2 * j + 2);
-                        } else {
-                            product(halves(w0, w1, pick), halves(w2, w3, pick), half, 2 * j);
-                        }
+                        low01[half] = halves(w0, w1, PAIRS ? LOW : pick); low23[half] = halves(w2, w3, PAIRS ? LOW : pick);
+                        if (PAIRS) { high01[half] = halves(w0, w1, HIGH); high23[half] = halves(w2, w3, HIGH); }
                     }
+                    product(low01, low23, 2 * j);
+                    if constexpr (PAIRS) product(high01, high23, 2 * j + 2);
+                }
             }
         }
         slot = slot + STAGE == G_RING * STAGE ? 0 : slot + STAGE;
@@ -734,22 +765,28 @@ Variant forward_kernel(int32_t H)
 template <int GB>
 Variant forward_of(bool f32, int N, int32_t H)
 {
-    Variant v = f32 ? forward_kernel<3, 1, GB, true>(H) : N > 16 ? forward_kernel<1, 4, GB, true>(H)
+    Variant v = f32 ? (N > 8 ? forward_kernel<3, 2, GB, true>(H) : forward_kernel<3, 1, GB, true>(H)) : N > 16 ? forward_kernel<1, 4, GB, true>(H)
               : N > 8 ? forward_kernel<1, 2, GB, true>(H) : forward_kernel<1, 1, GB, true>(H);
     if (v.smem > SMEM_MOST && !f32 && N > 16) v = forward_kernel<1, 2, GB, true>(H);
-    if (v.smem > SMEM_MOST && !f32) v = forward_kernel<1, 1, GB, true>(H);
+    if (v.smem > SMEM_MOST) v = f32 ? forward_kernel<3, 1, GB, true>(H) : forward_kernel<1, 1, GB, true>(H);
     if (v.smem <= SMEM_MOST) return v;
     return f32 ? forward_kernel<3, 1, GB, false>(H) : forward_kernel<1, 1, GB, false>(H);
 }
-template <int GB>
-Variant backward_of(bool f32, int N)
+template <int P, int GB, bool EXACT>
+Variant backward_kernel(int N)
 {
-    if (f32) return N <= 8 ? Variant{od_q4_grad_kernel<3, 1, GB>, grad_bytes<3, 1, GB>, 8, THREADS} : Variant{od_q4_grad_kernel<3, 2, GB>, grad_bytes<3, 2, GB>, 16, THREADS};
-    return N <= 8 ? Variant{od_q4_grad_kernel<2, 1, GB>, grad_bytes<2, 1, GB>, 8, THREADS} : Variant{od_q4_grad_kernel<2, 2, GB>, grad_bytes<2, 2, GB>, 16, THREADS};
+    if (N <= 8) return {od_q4_grad_kernel<P, 1, GB, EXACT>, grad_bytes<P, 1, GB>, 8, THREADS};
+    return {od_q4_grad_kernel<P, 2, GB, EXACT>, grad_bytes<P, 2, GB>, 16, THREADS};
 }
-Variant variant(bool backward, int32_t G, bool f32, int N, int32_t H)
+template <int GB>
+Variant backward_of(bool f32, bool exact, int N)
 {
-    if (backward) return G == 32 ? backward_of<1>(f32, N) : G == 64 ? backward_of<2>(f32, N) : backward_of<4>(f32, N);
+    if (exact) return f32 ? backward_kernel<3, GB, true>(N) : backward_kernel<2, GB, true>(N);
+    return f32 ? backward_kernel<3, GB, false>(N) : backward_kernel<2, GB, false>(N);
+}
+Variant variant(bool backward, int32_t G, bool f32, bool out_f32, int N, int32_t H)
+{
+    if (backward) return G == 32 ? backward_of<1>(f32, out_f32, N) : G == 64 ? backward_of<2>(f32, out_f32, N) : backward_of<4>(f32, out_f32, N);
     return G == 32 ? forward_of<1>(f32, N, H) : G == 64 ? forward_of<2>(f32, N, H) : forward_of<4>(f32, N, H);
 }
 
@@ -777,10 +814,10 @@ cudaError_t od_q4_prepare_device(int32_t *clusters)
     // (every variant: these sizes reach one, two, four parts of 8 tokens, rings of three and two stages, and none in shared memory)
     for (int backward = 0; backward < 2; ++backward)
         for (int32_t G = 32; G <= 128; G *= 2)
-            for (int f32 = 0; f32 < 2; ++f32)
+            for (int types = 0; types < 4; ++types)
                 for (int N = 8; N <= 32; N *= 2)
                     for (int32_t H = 128; H <= 65536; H += H < 16384 ? 128 : 49152) {
-                        const Variant v = variant(backward, G, f32, N, H);
+                        const Variant v = variant(backward, G, types & 1, types >> 1, N, H);
                         if (v.kernel == done) continue;
                         cudaError_t e = cudaFuncSetAttribute((const void *)v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST);
                         if (e == cudaSuccess && backward) e = cudaFuncSetAttribute((const void *)v.kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
@@ -788,7 +825,7 @@ cudaError_t od_q4_prepare_device(int32_t *clusters)
                         done = v.kernel;
                     }
     for (int n = 0; n <= OD_Q4_MAX_SPLIT; ++n) {           // (the variant with the most shared memory; each fills a multiprocessor)
-        const Variant v = variant(true, 32, true, 16, 128);
+        const Variant v = variant(true, 32, true, true, 16, 128);
         cudaLaunchConfig_t cfg = {};
         cudaLaunchAttribute attr[1];
         attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -813,7 +850,7 @@ cudaError_t od_launch_q4(const od_ctx *c, bool backward, int32_t N, int32_t V, i
     Q4Args args = {a, as, (const uint8_t *)codes, (const unsigned short *)scales, b, bs, N, V, H, f32, b_dtype == OD_F32,
                    H % COLS == 0 && ((uintptr_t)scales & 7u) == 0, 0x43004300u, 1, 1, 1, 0, 0, c->d_q4_parts};
     if (!backward) {
-        const Variant v = variant(false, G, f32, N, H);
+        const Variant v = variant(false, G, f32, false, N, H);
         const int64_t units = ((int64_t)V + ROWS - 1) / ROWS, blocks = units < sms ? units : sms;
         // Warps to the same 16 rows (1, 2, 4): the fewest stages in a row of one warp, of equal ones the fewest warps
         const int64_t each = (units + blocks - 1) / blocks, stages = (H + 32 * WIDE - 1) / (32 * WIDE);
@@ -826,7 +863,7 @@ cudaError_t od_launch_q4(const od_ctx *c, bool backward, int32_t N, int32_t V, i
     }
     // 16 tokens at a time, then 8: the scratch is for one time
     for (int32_t n = 0; n < N;) {
-        const Variant v = variant(true, G, f32, N - n, H);
+        const Variant v = variant(true, G, f32, b_dtype == OD_F32, N - n, H);
         // Warps side by side (4, 2, 1), blocks on the same columns (as many as there are multiprocessors for, or a cluster of
         // any size) and how these are joined, by the time that it takes in twentieths of a us, as measured: a stage of a warp 13, and
         // for every eight tokens 13, 6 for each group of its columns but one and 6 if they are fp32; the join 80, a cluster 20.
