@@ -224,6 +224,7 @@ __global__ void __launch_bounds__(THREADS, 4) od_score_kernel(const ScoreArgs A)
 {
     __shared__ float group_max[GROUPS];
     __shared__ Sums warp_sums[WARPS], block_sums[MAX_SPLIT];
+    __shared__ float block_ones[MAX_SPLIT];
     // candidates, and the best of all blocks of the row; maxima, and those that reach the bound (slot << 8 | thread)
     __shared__ __align__(16) Key cand[TOP ? CAP : 1], best[TOP ? MAX_SPLIT * OD_MAX_TOP : 1];
     __shared__ float maxima[TOP ? SLOTS : 1][THREADS];
@@ -315,6 +316,36 @@ __global__ void __launch_bounds__(THREADS, 4) od_score_kernel(const ScoreArgs A)
     const Sums w = warp_total(t, scale);
     if (lane == 0) warp_sums[warp] = w;
     __syncthreads();
+    const Sums nothing = {-FLT_MAX, 0.f, 0.f};
+    Sums all = warp_total(lane < WARPS ? warp_sums[lane] : nothing, scale);
+    // Where the largest logit has nearly all of the mass, what the others have is what the entropy and its log probability
+    // are made of, and behind the largest one's 1 its digits are lost: the thread that has read that one is summed again
+    // without it, and ones + s is the sum from here on.
+    const bool peaked = all.s >= 1.f && all.s < 1.0625f;
+    if (peaked) {
+        const unsigned has = __ballot_sync(0xFFFFFFFFu, t.c == all.c && t.s >= 1.f);
+        if (has) {                                         // (one lane of one warp)
+            float rest = 0.f;
+            for (int i = lo + warp * 32 + __ffs(has) - 1 + lane * THREADS; i < hi; i += 32 * THREADS) {
+                const uint4 v = load_vec<DTYPE>(row, i, V);
+#pragma unroll
+                for (int k = 0; k < VEC<DTYPE>; ++k) {
+                    const float e = element<DTYPE>(v, k);
+                    if (e < all.c) rest += od_ex2((e - all.c) * scale);
+                }
+            }
+            if (!(has >> lane & 1)) {
+                Sums mine = t;
+                mine.raise(all.c, scale);
+                rest += mine.s;
+            }
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) rest += __shfl_xor_sync(0xFFFFFFFFu, rest, o);
+            if (lane == 0) warp_sums[warp].s = rest;
+        }
+        __syncthreads();
+        all = warp_total(lane < WARPS ? warp_sums[lane] : nothing, scale);
+    }
     if (TOP) {
         // the bound: the largest logit of the group that has n - 1 others in front of it
         const float g = group_max[lane];
@@ -414,18 +445,29 @@ __global__ void __launch_bounds__(THREADS, 4) od_score_kernel(const ScoreArgs A)
         od_cluster_wait();
     }
     // the parts of the row to its cluster's first block
-    Sums all = {-FLT_MAX, 0.f, 0.f};
-    if (lane < WARPS) all = warp_sums[lane];
-    all = warp_total(all, scale);
     if (tid < 3) store_cluster((float *)(block_sums + part) + tid, 0, tid == 0 ? all.c : tid == 1 ? all.s : all.a);
+    if (tid == 3) store_cluster(block_ones + part, 0, peaked ? 1.f : 0.f);
     od_cluster_arrive();
     if (part != 0) return;                                 // (nobody writes into this block)
     od_cluster_wait();
-    all = {-FLT_MAX, 0.f, 0.f};
-    if (lane < (int)split) all = block_sums[lane];
-    all = warp_total(all, scale);
+    float ones = 0.f;
+    {
+        Sums of = nothing;
+        if (lane < (int)split) { of = block_sums[lane]; ones = block_ones[lane]; }
+        float c = of.c;
+#pragma unroll
+        for (int o = 1; o < MAX_SPLIT; o <<= 1) c = fmaxf(c, __shfl_xor_sync(0xFFFFFFFFu, c, o));
+        c = __shfl_sync(0xFFFFFFFFu, c, 0);
+        if (of.c < c) { of.s += ones; ones = 0.f; }        // (a one of another largest logit is none of the row's)
+        all = warp_total(of, scale);
+#pragma unroll
+        for (int o = 1; o < MAX_SPLIT; o <<= 1) ones += __shfl_xor_sync(0xFFFFFFFFu, ones, o);
+        ones = __shfl_sync(0xFFFFFFFFu, ones, 0);
+    }
+    const float rest = all.s;
+    all.s += ones;
     const bool finite = all.s == all.s, empty = all.s == 0.f;
-    const float nan = __int_as_float(0x7FFFFFFF), ln_s = logf(all.s);
+    const float nan = __int_as_float(0x7FFFFFFF), ln_s = ones == 1.f ? log1pf(rest) : logf(all.s);
     if (tid == 0) {
         A.row_max[r] = !finite ? nan : empty ? -INFINITY : all.c;
         A.row_sum[r] = all.s;

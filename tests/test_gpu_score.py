@@ -386,6 +386,31 @@ def test_scores_of_a_step(ctx):
     c.close()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,V", [(1, 32000), (1, 7), (3, 152064), (500, 4099)])
+def test_rows_with_nearly_all_mass_on_one_token(ctx, rows, V, dtype):
+    """Entropies and log probabilities near zero keep their digits: they are sums of the other terms alone, each within
+    2^-22 + 3 * 2^-24 |(x - M) / T| of its value, below 2^-16 with |(x - M) / T| up to 70, and of their products with that."""
+    g = torch.Generator(device="cuda").manual_seed(18)
+    x = torch.randn(rows, 1, V, generator=g, device="cuda")
+    at = torch.randint(0, V, (rows,), generator=g, device="cuda")
+    x[torch.arange(rows), 0, at] = 14.0 + 12.0 * torch.rand(rows, generator=g, device="cuda")
+    x = padded(x.to(dtype))
+    T = torch.full((rows,), 0.7, device="cuda")
+    ids = at.int()[:, None]
+    out = od.od_token_logprobs(ctx, x, ids, T, n_top=1)
+    ref = reference(x, ids, T, 1)
+    d = torch.where(ref["z"] == 0, -torch.inf, ref["z"])    # without the largest
+    rest = torch.exp(d).sum(2)
+    less = -(torch.exp(d) * torch.where(d > -torch.inf, d, 0.0)).sum(2)
+    want_h = torch.log1p(rest) + less / (1 + rest)
+    assert torch.equal(out.top_ids[:, :, 0].long(), at[:, None])
+    same(out.logprob, -torch.log1p(rest), 2.0 ** -16 * rest)
+    same(out.top_logprobs[:, :, 0], -torch.log1p(rest), 2.0 ** -16 * rest)
+    same(out.entropy, want_h, 2.0 ** -15 * want_h)
+    same(out.row_sum, 1 + rest, E * (1 + rest))
+
+
 def test_long_rows_of_many(ctx):
     """A block to a row and more turns of a thread than it leaves maxima."""
     B, V, n = 300, 300007, 20
