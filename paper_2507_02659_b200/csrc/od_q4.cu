@@ -852,11 +852,13 @@ cudaError_t od_launch_q4(const od_ctx *c, bool backward, int32_t N, int32_t V, i
     if (!backward) {
         const Variant v = variant(false, G, f32, false, N, H);
         const int64_t units = ((int64_t)V + ROWS - 1) / ROWS, blocks = units < sms ? units : sms;
-        // Warps to the same 16 rows (1, 2, 4): the fewest stages in a row of one warp, of equal ones the fewest warps
+        // Warps to the same 16 rows (1, 2, 4), by the time of a warp's turns: its stages, and for the sums to be joined as much as
+        // one stage more, or of four warps three. (us, 1 / 2 / 4: 8 tokens through 128256 x 4096 59 / 52 / 57, 2000 x 4096
+        // 10.9 / 8.1 / 6.7, 4 through 152064 x 2048 34 / 36 / 43, 8 through 64000 x 1024 12.7 / 12.7 / 16.9.)
         const int64_t each = (units + blocks - 1) / blocks, stages = (H + 32 * WIDE - 1) / (32 * WIDE);
         int64_t best = INT64_MAX;
         for (int32_t ks = 1; ks <= 4 && ks <= stages; ks *= 2) {
-            const int64_t cost = (each * ks + F_WARPS - 1) / F_WARPS * ((stages + ks - 1) / ks);
+            const int64_t cost = (each * ks + F_WARPS - 1) / F_WARPS * ((stages + ks - 1) / ks + ks - 1);
             if (cost < best) { best = cost; args.k_split = ks; }
         }
         return launch(v.kernel, dim3((unsigned)blocks, (unsigned)((N + v.tokens - 1) / v.tokens)), F_THREADS, v.smem, 1, pdl, s, args);
