@@ -8,24 +8,27 @@
 // Everything is held in fp32. Differences from the running maximum are formed before they are scaled: x T^-1 may
 // overflow (a mask of the type's lowest value) or lose the digits that the exponential is made of, x - M does not.
 //
-// Forward: one pass. A block of 256 threads (or a cluster of them: one contiguous slice of the row to each) keeps, per
+// Forward: one pass. A block of 128 or 256 threads (or a cluster of them: one contiguous slice of the row to each) keeps, per
 // thread, the maximum, the sum of e and the sum of e (x - M), raised to a new maximum once per four 16-byte loads.
-// The alternatives cost next to nothing in that pass: the largest logits of 32 groups of eight threads are 32 different
+// The alternatives cost next to nothing in that pass: the largest logits of 32 groups of threads are 32 different
 // elements, so the n-th largest of them is a bound that at least n elements of the slice reach and few more do. Threads leave
 // the maximum of every four loads in shared memory: only loads whose maximum reaches the bound are looked at again (from L2,
 // all of them at once), and what reaches the bound is ranked by counting.
 //
 // Backward: elementwise, one read and one write; the given token and the alternatives are written over the dense
 // values of their chunk behind a block barrier.
+//
+// Measured (us; HBM's rate for the bytes): scores of 4608 rows of 152064 bf16 logits with one alternative 242 (217), without
+// 226; 96 rows of 128256 with 20 16 (3.8: launch, a row's chain of barriers, its alternatives); gradient of 448 rows of 128256,
+// 256 of which count, 32 (28). The large ones are at HBM's rate but for a row's end, the small ones at their chain.
 #include <float.h>
 
 #include "od_common.cuh"
 
 namespace {
 
-constexpr int THREADS = 256;
+constexpr int THREADS = 256;                               // (of the scores' blocks also half as many)
 constexpr int WARPS = THREADS / 32;
-constexpr int GROUPS = THREADS / 8;                        // of eight threads
 constexpr int U = 4;                                       // 16-byte loads of a thread in flight
 constexpr int MAX_SPLIT = 8;                               // blocks of a row (a portable cluster)
 constexpr int CAP = 512;                                   // candidates that are ranked by counting
@@ -34,8 +37,6 @@ constexpr int SLOTS = 32;                                  // maxima that a thre
 constexpr int AGAIN = 256;                                 // of them that are looked at again
 constexpr float LEAST = -150.f;                            // exp2 of it is zero
 constexpr float LN2 = 0.69314718055994531f, LOG2E = 1.4426950408889634f;
-static_assert(GROUPS == 32, "a group to each lane");
-static_assert(MAX_SPLIT * OD_MAX_TOP <= THREADS, "a thread to each alternative of the blocks");
 static_assert(WARPS * OD_MAX_TOP <= CAP, "a list from every warp fits");
 
 struct ScoreArgs {
@@ -219,10 +220,11 @@ __device__ __forceinline__ Sums warp_total(Sums t, float scale)
 // (a temperature whose reciprocal overflows is none)
 __device__ __forceinline__ bool usable(float T) { return T > 0.f && T < INFINITY && LOG2E / T < INFINITY; }
 
-template <int DTYPE, bool TOP>
-__global__ void __launch_bounds__(THREADS, 4) od_score_kernel(const ScoreArgs A)
+template <int DTYPE, bool TOP, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) od_score_kernel(const ScoreArgs A)
 {
-    __shared__ float group_max[GROUPS];
+    constexpr int WARPS = THREADS / 32, GROUP = THREADS / 32;  // threads to one of 32 groups
+    __shared__ float group_max[32];
     __shared__ Sums warp_sums[WARPS], block_sums[MAX_SPLIT];
     __shared__ float block_ones[MAX_SPLIT];
     // candidates, and the best of all blocks of the row; maxima, and those that reach the bound (slot << 8 | thread)
@@ -310,8 +312,8 @@ __global__ void __launch_bounds__(THREADS, 4) od_score_kernel(const ScoreArgs A)
     if (TOP) {
         float g = t.c;
 #pragma unroll
-        for (int o = 1; o < 8; o <<= 1) g = fmaxf(g, __shfl_xor_sync(0xFFFFFFFFu, g, o));
-        if ((lane & 7) == 0) group_max[tid >> 3] = g;
+        for (int o = 1; o < GROUP; o <<= 1) g = fmaxf(g, __shfl_xor_sync(0xFFFFFFFFu, g, o));
+        if (tid % GROUP == 0) group_max[tid / GROUP] = g;
     }
     const Sums w = warp_total(t, scale);
     if (lane == 0) warp_sums[warp] = w;
@@ -351,7 +353,7 @@ __global__ void __launch_bounds__(THREADS, 4) od_score_kernel(const ScoreArgs A)
         const float g = group_max[lane];
         int rank = 0;
 #pragma unroll
-        for (int k = 0; k < GROUPS; ++k) rank += group_max[k] > g || (group_max[k] == g && k < lane);
+        for (int k = 0; k < 32; ++k) rank += group_max[k] > g || (group_max[k] == g && k < lane);
         const float bound = __shfl_sync(0xFFFFFFFFu, g, __ffs(__ballot_sync(0xFFFFFFFFu, rank == n - 1)) - 1);
         // by whole warps: a place for what reaches the bound (which is at least -FLT_MAX) in N vectors of each lane
         auto offer = [&](const uint4 *x, const int *at, int N) {
@@ -484,8 +486,8 @@ __global__ void __launch_bounds__(THREADS, 4) od_score_kernel(const ScoreArgs A)
             return;
         }
         // the blocks' lists are in order: a key's place is the sum of its places in all of them
-        if (tid < (int)split * n) {                        // (at most THREADS)
-            const Key k = best[tid];
+        for (int j = tid; j < (int)split * n; j += THREADS) {
+            const Key k = best[j];
             int at[MAX_SPLIT] = {};
 #pragma unroll
             for (int o = OD_MAX_TOP; o > 0; o >>= 1) {
@@ -667,10 +669,10 @@ __global__ void __launch_bounds__(THREADS) od_score_grad_kernel(const ScoreGradA
 }
 
 template <typename K, typename A>
-cudaError_t launch(K kernel, unsigned blocks, unsigned cluster, bool pdl, const A &args, cudaStream_t s)
+cudaError_t launch(K kernel, unsigned blocks, unsigned cluster, bool pdl, const A &args, cudaStream_t s, unsigned threads = THREADS)
 {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(blocks); cfg.blockDim = dim3(THREADS);
+    cfg.gridDim = dim3(blocks); cfg.blockDim = dim3(threads);
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -700,9 +702,18 @@ cudaError_t od_launch_score(const od_ctx *c, int32_t B, int32_t R, int32_t V, co
                          logprob, entropy, row_max, row_sum, top_logprobs, top_ids, flags};
     const unsigned blocks = (unsigned)(rows * split);
     const bool pdl = c->opt_pdl != 0;
+    // Threads of a block that has a row alone: half as many where rows are short or more than are resident at a time, so that
+    // more rows are, and one's end lies under others' loads. (us with one alternative, 256 / 128 threads: 2200 rows of 32000
+    // bf16 logits 49 / 42, 4608 of 152064 258 / 242, 1000 of 4000 17 / 11; but 448 of 128256 34 / 37.)
+    const bool half = split == 1 && (rows > 4 * c->sm_count || (int64_t)V * esz <= 96 * 1024);
+    const auto of = [&](auto whole_block, auto half_block) {
+        return half ? launch(half_block, blocks, 1, pdl, a, s, THREADS / 2) : launch(whole_block, blocks, split, pdl, a, s);
+    };
     if (dtype == OD_BF16)
-        return n_top ? launch(od_score_kernel<OD_BF16, true>, blocks, split, pdl, a, s) : launch(od_score_kernel<OD_BF16, false>, blocks, split, pdl, a, s);
-    return n_top ? launch(od_score_kernel<OD_F32, true>, blocks, split, pdl, a, s) : launch(od_score_kernel<OD_F32, false>, blocks, split, pdl, a, s);
+        return n_top ? of(od_score_kernel<OD_BF16, true, THREADS>, od_score_kernel<OD_BF16, true, THREADS / 2>)
+                     : of(od_score_kernel<OD_BF16, false, THREADS>, od_score_kernel<OD_BF16, false, THREADS / 2>);
+    return n_top ? of(od_score_kernel<OD_F32, true, THREADS>, od_score_kernel<OD_F32, true, THREADS / 2>)
+                 : of(od_score_kernel<OD_F32, false, THREADS>, od_score_kernel<OD_F32, false, THREADS / 2>);
 }
 
 // Loads of a thread: up to 8, as long as there are eight blocks for every multiprocessor
