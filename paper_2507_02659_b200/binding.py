@@ -530,7 +530,7 @@ def _q4(ctx: Context, x, codes, scales, out, dtype, backward: bool):
             _check(status, name)
             return out
     d = ctx.device
-    V, H = int(codes.shape[0]), int(codes.shape[1]) * 2
+    V, H = (int(codes.shape[0]), int(codes.shape[1]) * 2) if codes.dim() == 2 else (0, 0)
     if codes.dim() != 2 or scales.dim() != 2 or scales.shape[0] != V or scales.shape[1] < 1 or H % scales.shape[1]:
         raise ValueError("codes must be [V, H / 2] and scales [V, H / group]")
     wide, wide_out = (V, H) if backward else (H, V)

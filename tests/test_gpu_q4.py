@@ -299,6 +299,17 @@ def test_refusals(ctx):
     assert od.od_q4_logits_grad(ctx, torch.zeros(0, 100, device="cuda"), codes, scales).shape == (0, 128)
 
 
+@pytest.mark.parametrize("call", [od.od_q4_logits, od.od_q4_logits_grad])
+@pytest.mark.parametrize("given", [False, True])
+def test_refuses_weights_of_other_dimensions(ctx, call, given):
+    codes, scales = layer(128, 128, 32, 9)
+    x = torch.randn(2, 128, device="cuda")
+    out = torch.empty(2, 128, device="cuda") if given else None
+    for c, s in [(codes.view(-1), scales), (codes[None], scales), (codes, scales.view(-1)), (codes, scales[None])]:
+        with pytest.raises(ValueError):
+            call(ctx, x, c, s, out=out)
+
+
 def test_scales_far_from_one(ctx):
     """Scales that cannot be scaled up with the rest, and tiny ones, next to usual ones: groups of either kind in both directions."""
     N, V, H, G = 9, 70, 256, 64
