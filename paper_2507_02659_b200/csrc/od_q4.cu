@@ -22,9 +22,10 @@
 // up: without the arithmetic the forward kernel reads 6.2 TB/s. Sixteen-byte pieces are placed so that the words of a
 // fragment lie in different banks.
 //
-// Measured (us; codes and scales / HBM's rate): forward 8 tokens, 128256 x 4096 in groups of 128: 52 (42); backward 8
-// positions, 128256 x 2048: 42 (21), 16: 62. What bounds both now is issue: masks share their dispatch with the matrix
-// instructions (ncu: masks' pipe 58 %, tensor pipe 31 % forward; 56 % and 40 % backward).
+// Measured (us; codes and scales / HBM's rate): forward 8 tokens, 128256 x 4096 in groups of 128: 52 (42), and 60 in a long
+// run, under the power cap; backward 8 positions, 128256 x 2048: 44 (21), 16: 68, with fp32 results 47 and 81. What bounds both
+// now is issue: masks share their dispatch with the matrix instructions (ncu: masks' pipe 56 %, tensor pipe 30 % forward; 56 %
+// and 37 % backward).
 #include <float.h>
 
 #include "od_common.cuh"
@@ -463,7 +464,7 @@ __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
 //
 // Rows are summed over: two of them are the pair of an operand, four columns in a row are a half word. The tokens' side is
 // made anew for each group: gradient times scale, in pieces. The codes are brought to u - 8 here, as ordinary bf16 numbers
-// (two shifts or masks more and a subtraction for two codes, 5 % of the time). Gradients have mostly one sign (a softmax but
+// (two shifts or masks more and a subtraction for two codes: 44 us for 41 with eight positions, 112 for 101 with 24). Gradients have mostly one sign (a softmax but
 // for one large entry), and where sums of them with 0 to 15 were taken the tensor pipe's cuts were 1e-5 of the result; with
 // numbers below bf16's normal ones, which the pipe lines up as if their leading bits were there, 1e-6; so they are 4e-7, and
 // of fp32 results 2e-7 (EXACT below), where plain fp32 sums are 5e-7 off.
@@ -753,7 +754,7 @@ struct Variant { Kernel kernel; int smem, tokens, threads; };
 // Forward: 8, 16 or 32 tokens to a block, the most (and no more than there are) whose inputs fit into shared memory
 // beside the rings; where those of 8 do not, they stay in global memory. Backward: 8 or 16.
 // The ring of a warp has three stages, or two where the tokens' fragments fit with two only (16 tokens of 4096 columns,
-// 32000 rows: 26 us, and 34 eight at a time).
+// 32000 rows: 24 us, and 34 eight at a time).
 constexpr int SMEM_MOST = 226 * 1024;                      // (and a little of fixed size)
 template <int P, int NT, int GB, bool XS>
 Variant forward_kernel(int32_t H)
