@@ -23,7 +23,7 @@
 // fragment lie in different banks.
 //
 // Measured (us; codes and scales / HBM's rate): forward 8 tokens, 128256 x 4096 in groups of 128: 52 (42), and 60 in a long
-// run, under the power cap; backward 8 positions, 128256 x 2048: 44 (21), 16: 68, with fp32 results 47 and 81. What bounds both
+// run, under the power cap; backward 8 positions, 128256 x 2048: 44 (21), 16: 63, 24: 85, 32: 105, with fp32 results 47, 71, 103 and 115. What bounds both
 // now is issue: masks share their dispatch with the matrix instructions (ncu: masks' pipe 56 %, tensor pipe 30 % forward; 56 %
 // and 37 % backward).
 #include <float.h>
@@ -32,10 +32,13 @@
 
 namespace {
 
-constexpr int WARPS = 16, THREADS = 32 * WARPS;
 constexpr int F_WARPS = 16, F_THREADS = 32 * F_WARPS;
 constexpr int ROWS = 16;                                   // of a matrix instruction
 constexpr int COLS = 128;                                  // backward: of a warp, four blocks of 32
+// Backward: warps of a block, by eights of tokens. A warp's sums are 32 numbers of a lane for every eight tokens: with fewer warps
+// codes are unpacked for more tokens at once. (128256 x 2048, us to bf16 results: 16 tokens by 16 / 12 / 8 warps 69 / 63 / 68; 24 by 8 / 10
+// 85 / 98, and 113 as 16 and then 8; 32 by 8 / 10 105 / 136; 8 by 16 / 12 45 / 46.)
+constexpr int G_WARPS[5] = {0, 16, 12, 8, 8};
 constexpr int G_RING = 3;                                  // backward: stages of a warp
 constexpr int WIDE = 8;                                    // forward: blocks of 32 columns to a stage
 constexpr int WIDE_STAGE = ROWS * WIDE * 16;              // bytes
@@ -464,7 +467,7 @@ __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
 //
 // Rows are summed over: two of them are the pair of an operand, four columns in a row are a half word. The tokens' side is
 // made anew for each group: gradient times scale, in pieces. The codes are brought to u - 8 here, as ordinary bf16 numbers
-// (two shifts or masks more and a subtraction for two codes: 44 us for 41 with eight positions, 112 for 101 with 24). Gradients have mostly one sign (a softmax but
+// (two shifts or masks more and a subtraction for two codes: 44 us for 41 with eight positions). Gradients have mostly one sign (a softmax but
 // for one large entry), and where sums of them with 0 to 15 were taken the tensor pipe's cuts were 1e-5 of the result; with
 // numbers below bf16's normal ones, which the pipe lines up as if their leading bits were there, 1e-6; so they are 4e-7, and
 // of fp32 results 2e-7 (EXACT below), where plain fp32 sums are 5e-7 off.
@@ -485,11 +488,12 @@ template <int P, int NT, int GB> constexpr int g_warp = G_RING * g_stage<P, NT> 
 // EXACT, for fp32 results: the tensor pipe cuts what it adds to its accumulators (to 2^-23 of the largest), so what it adds up in a
 // stage begins at zero and is then added to the sums in fp32 as such, which rounds (128256 x 1824, 28 positions: 2e-6 of the
 // result otherwise, where plain fp32 sums are 7e-7 off).
-template <int P, int NT, int GB, bool EXACT>
-__global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
+template <int P, int NT, int GB, bool EXACT, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS, 1) od_q4_grad_kernel(const Q4Args A)
 {
     extern __shared__ __align__(128) unsigned char smem[];
     constexpr bool F32 = P == 3;
+    constexpr int THREADS = 32 * WARPS;
     constexpr int ESZ = F32 ? 4 : 2, GROUPS = 4 / GB, PIECES = G_ROWS * ESZ / 16, STAGE = g_stage<P, NT>;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -571,7 +575,7 @@ __global__ void __launch_bounds__(THREADS, 1) od_q4_grad_kernel(const Q4Args A)
         cp_wait<G_RING - 2>();
         __syncwarp();
         fetch();
-        // of eight tokens both halves of the rows side by side, for what can run at the same time; of sixteen registers lack
+        // of eight tokens both halves of the rows side by side, for what can run at the same time; of more registers lack
         constexpr int SIDE = NT == 1 ? 2 : 1;
 #pragma unroll
         for (int base = 0; base < 2; base += SIDE) {
@@ -746,13 +750,13 @@ __global__ void __launch_bounds__(32 * JOIN) od_q4_join_kernel(const Q4Args A, i
 }
 
 template <int NT> constexpr int part_bytes = F_WARPS * NT * 512;
-template <int P, int NT, int GB> constexpr int grad_bytes = WARPS * (g_warp<P, NT, GB> > 8 * NT * COLS * 4 ? g_warp<P, NT, GB> : 8 * NT * COLS * 4);
+template <int P, int NT, int GB, int WARPS> constexpr int grad_bytes = WARPS * (g_warp<P, NT, GB> > 8 * NT * COLS * 4 ? g_warp<P, NT, GB> : 8 * NT * COLS * 4);
 
 typedef void (*Kernel)(Q4Args);
 struct Variant { Kernel kernel; int smem, tokens, threads; };
 
 // Forward: 8, 16 or 32 tokens to a block, the most (and no more than there are) whose inputs fit into shared memory
-// beside the rings; where those of 8 do not, they stay in global memory. Backward: 8 or 16.
+// beside the rings; where those of 8 do not, they stay in global memory. Backward: 8, 16, 24 or 32.
 // The ring of a warp has three stages, or two where the tokens' fragments fit with two only (16 tokens of 4096 columns,
 // 32000 rows: 24 us, and 34 eight at a time).
 constexpr int SMEM_MOST = 226 * 1024;                      // (and a little of fixed size)
@@ -773,11 +777,17 @@ Variant forward_of(bool f32, int N, int32_t H)
     if (v.smem <= SMEM_MOST) return v;
     return f32 ? forward_kernel<3, 1, GB, false>(H) : forward_kernel<1, 1, GB, false>(H);
 }
+template <int P, int NT, int GB, bool EXACT>
+Variant backward_for()
+{
+    constexpr int W = G_WARPS[NT];
+    return {od_q4_grad_kernel<P, NT, GB, EXACT, W>, grad_bytes<P, NT, GB, W>, 8 * NT, 32 * W};
+}
 template <int P, int GB, bool EXACT>
 Variant backward_kernel(int N)
 {
-    if (N <= 8) return {od_q4_grad_kernel<P, 1, GB, EXACT>, grad_bytes<P, 1, GB>, 8, THREADS};
-    return {od_q4_grad_kernel<P, 2, GB, EXACT>, grad_bytes<P, 2, GB>, 16, THREADS};
+    return N <= 8 ? backward_for<P, 1, GB, EXACT>() : N <= 16 ? backward_for<P, 2, GB, EXACT>()
+         : N <= 24 ? backward_for<P, 3, GB, EXACT>() : backward_for<P, 4, GB, EXACT>();
 }
 template <int GB>
 Variant backward_of(bool f32, bool exact, int N)
@@ -816,7 +826,7 @@ cudaError_t od_q4_prepare_device(int32_t *clusters)
     for (int backward = 0; backward < 2; ++backward)
         for (int32_t G = 32; G <= 128; G *= 2)
             for (int types = 0; types < 4; ++types)
-                for (int N = 8; N <= 32; N *= 2)
+                for (int N = 8; N <= 32; N += 8)
                     for (int32_t H = 128; H <= 65536; H += H < 16384 ? 128 : 49152) {
                         const Variant v = variant(backward, G, types & 1, types >> 1, N, H);
                         if (v.kernel == done) continue;
@@ -826,7 +836,7 @@ cudaError_t od_q4_prepare_device(int32_t *clusters)
                         done = v.kernel;
                     }
     for (int n = 0; n <= OD_Q4_MAX_SPLIT; ++n) {           // (the variant with the most shared memory; each fills a multiprocessor)
-        const Variant v = variant(true, 32, true, true, 16, 128);
+        const Variant v = variant(true, 32, true, true, 8, 128);
         cudaLaunchConfig_t cfg = {};
         cudaLaunchAttribute attr[1];
         attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -864,30 +874,31 @@ cudaError_t od_launch_q4(const od_ctx *c, bool backward, int32_t N, int32_t V, i
         }
         return launch(v.kernel, dim3((unsigned)blocks, (unsigned)((N + v.tokens - 1) / v.tokens)), F_THREADS, v.smem, 1, pdl, s, args);
     }
-    // 16 tokens at a time, then 8: the scratch is for one time
+    // 32 tokens at a time, then what is left: the scratch is for one time
     for (int32_t n = 0; n < N;) {
         const Variant v = variant(true, G, f32, b_dtype == OD_F32, N - n, H);
         // Warps side by side (4, 2, 1), blocks on the same columns (as many as there are multiprocessors for, or a cluster of
-        // any size) and how these are joined, by the time that it takes in twentieths of a us, as measured: a stage of a warp 13, and
+        // any size) and how these are joined, by the time that it takes in twentieths of a us, as measured with 16 warps (in proportion to them it chose no better): a stage of a warp 13, and
         // for every eight tokens 13, 6 for each group of its columns but one and 6 if they are fp32; the join 80, a cluster 20.
         // Of equal ones the widest rows.
         const int64_t steps = ((int64_t)V + G_ROWS - 1) / G_ROWS, stage = 13 + v.tokens / 8 * (13 + 6 * (128 / G - 1) + 6 * f32);
         int64_t best = INT64_MAX, blocks = 0;
+        const int warps = v.threads / 32;
         auto offer = [&](int32_t cw, int64_t split, int64_t rounds, int64_t join, bool cluster) {
-            const int64_t slabs = split * (WARPS / cw), cost = rounds * ((steps + slabs - 1) / slabs) * stage + join;
+            const int64_t slabs = split * (warps / cw), cost = rounds * ((steps + slabs - 1) / slabs) * stage + join;
             if (cost >= best) return;
             best = cost; blocks = (H + cw * COLS - 1) / (cw * COLS) * split;
             args.col_warps = cw; args.split = (int32_t)split; args.cluster = cluster;
         };
         for (int32_t cw = 4 * 8 / v.tokens; cw >= 1; cw /= 2) {
-            const int64_t tiles = (H + cw * COLS - 1) / (cw * COLS), deep = WARPS / cw, most = (steps + deep - 1) / deep;
+            const int64_t tiles = (H + cw * COLS - 1) / (cw * COLS), deep = warps / cw, most = (steps + deep - 1) / deep;
             const int64_t split = tiles > sms ? 1 : sms / tiles < most ? sms / tiles : most;
             offer(cw, split, (tiles * split + sms - 1) / sms, split > 1 ? 80 : 0, false);
             for (int32_t k = 2; k <= OD_Q4_MAX_SPLIT && k <= most; ++k)
                 if (c->q4_clusters[k] > 0) offer(cw, k, (tiles + c->q4_clusters[k] - 1) / c->q4_clusters[k], 20, true);
         }
         args.first_token = n;
-        cudaError_t e = launch(v.kernel, dim3((unsigned)blocks), THREADS, v.smem, args.cluster ? args.split : 1, pdl, s, args);
+        cudaError_t e = launch(v.kernel, dim3((unsigned)blocks), v.threads, v.smem, args.cluster ? args.split : 1, pdl, s, args);
         if (e == cudaSuccess && args.split > 1 && !args.cluster)
             e = launch(od_q4_join_kernel, dim3((unsigned)(H / 32), (unsigned)(N - n < v.tokens ? N - n : v.tokens)), dim3(32, JOIN), 0, 1, pdl, s, args, v.tokens);
         if (e != cudaSuccess) return e;

@@ -109,6 +109,14 @@ def test_gradient(ctx, N, V, H, G, given, made):
     assert torch.equal(out, od.od_q4_logits_grad(ctx, dy, codes, scales, dtype=made))
 
 
+# positions: about what one launch takes, and of several; short layers and ones that a second kernel joins
+@pytest.mark.parametrize("given,made", TYPES)
+@pytest.mark.parametrize("N,V,H,G", [(23, 40, 128, 32), (24, 3001, 1152, 64), (25, 517, 640, 32), (31, 33, 2048, 128), (32, 20003, 256, 32),
+                                     (40, 4100, 1024, 128), (41, 700, 96, 32), (56, 1000, 2048, 64)])
+def test_gradient_of_more_positions(ctx, N, V, H, G, given, made):
+    test_gradient(ctx, N, V, H, G, given, made)
+
+
 def test_every_code_and_column(ctx):
     """Unit vectors read single weights: every code at every place of a word, each group's own scale."""
     V, H, G = 16, 256, 64

@@ -149,10 +149,10 @@ def without_clusters():
 
 
 def test_the_gradients_join(without_clusters):
-    """Where blocks that are no cluster share columns a second kernel joins them, 16 tokens at a time and what is left."""
+    """Where blocks that are no cluster share columns a second kernel joins them, 32 tokens at a time and what is left."""
     lib = Lib()
-    assert lib.q4(N=24, V=32000, H=2048, backward=True) == OK
+    assert lib.q4(N=40, V=32000, H=2048, backward=True) == OK
     got = lib.log()
     assert len(got) == 4 and all(b <= 148 and y == 1 for _, b, y in got[0::2])
-    assert [x[1:] for x in got[1::2]] == [(2048 // 32, 16), (2048 // 32, 8)]
+    assert [x[1:] for x in got[1::2]] == [(2048 // 32, 32), (2048 // 32, 8)]
     lib.close()
