@@ -226,7 +226,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) od_score_kernel(const
     constexpr int WARPS = THREADS / 32, GROUP = THREADS / 32;  // threads to one of 32 groups
     __shared__ float group_max[32];
     __shared__ Sums warp_sums[WARPS], block_sums[MAX_SPLIT];
-    __shared__ float block_ones[MAX_SPLIT];
+    __shared__ float block_ones[MAX_SPLIT], peak_rest;
+    __shared__ int peak_warp;
     // candidates, and the best of all blocks of the row; maxima, and those that reach the bound (slot << 8 | thread)
     __shared__ __align__(16) Key cand[TOP ? CAP : 1], best[TOP ? MAX_SPLIT * OD_MAX_TOP : 1];
     __shared__ float maxima[TOP ? SLOTS : 1][THREADS];
@@ -319,10 +320,11 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) od_score_kernel(const
     if (lane == 0) warp_sums[warp] = w;
     __syncthreads();
     const Sums nothing = {-FLT_MAX, 0.f, 0.f};
-    Sums all = warp_total(lane < WARPS ? warp_sums[lane] : nothing, scale);
+    Sums of_warp = lane < WARPS ? warp_sums[lane] : nothing, all = warp_total(of_warp, scale);
     // Where the largest logit has nearly all of the mass, what the others have is what the entropy and its log probability
     // are made of, and behind the largest one's 1 its digits are lost: the thread that has read that one is summed again
-    // without it, and ones + s is the sum from here on.
+    // without it, and ones + s is the sum from here on. (Its warp's sum goes to a place of its own: other warps may still
+    // be reading warp_sums, by which all of them decide the same.)
     const bool peaked = all.s >= 1.f && all.s < 1.0625f;
     if (peaked) {
         const unsigned has = __ballot_sync(0xFFFFFFFFu, t.c == all.c && t.s >= 1.f);
@@ -343,10 +345,11 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) od_score_kernel(const
             }
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) rest += __shfl_xor_sync(0xFFFFFFFFu, rest, o);
-            if (lane == 0) warp_sums[warp].s = rest;
+            if (lane == 0) { peak_rest = rest; peak_warp = warp; }
         }
         __syncthreads();
-        all = warp_total(lane < WARPS ? warp_sums[lane] : nothing, scale);
+        if (lane == peak_warp) of_warp.s = peak_rest;
+        all = warp_total(of_warp, scale);
     }
     if (TOP) {
         // the bound: the largest logit of the group that has n - 1 others in front of it

@@ -483,3 +483,27 @@ def test_refusals(ctx):
         od.od_token_logprobs(ctx, x[0], ids[:1], T[:1], n_top=2, out=od.alloc_logprob_out(ctx, 1, 3, 2))
     assert od.od_token_logprobs(ctx, x[:0], ids[:0], T[:0], n_top=2).logprob.shape == (0, 3)
     np.testing.assert_array_equal(od.od_token_logprobs(ctx, x, ids, T, n_top=2).top_ids.cpu(), out.top_ids.cpu())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n", [0, 4])
+@pytest.mark.parametrize("rows,V", [(1, 40), (1, 152064), (40, 152064), (100, 152064), (200, 60000), (400, 130001), (700, 4099), (1300, 300)])
+def test_rows_with_nearly_all_mass_on_one_token_are_the_same_in_every_run(ctx, rows, V, n, dtype):
+    """Every warp of a block decides by the same sums that one token has nearly all of the mass, whichever of them holds it: one to
+    eight blocks a row, of either size, with such rows beside ordinary ones. The bounds of the test above."""
+    g = torch.Generator(device="cuda").manual_seed(19)
+    x = torch.randn(rows, 1, V, generator=g, device="cuda")
+    at = torch.randint(0, V, (rows,), generator=g, device="cuda")
+    peak = torch.arange(rows, device="cuda") % 4 != 3
+    x[torch.arange(rows), 0, at] = torch.where(peak, 16.0 + 10.0 * torch.rand(rows, generator=g, device="cuda"), 1.0)
+    x = padded(x.to(dtype))
+    T = torch.full((rows,), 0.7, device="cuda")
+    ids = at.int()[:, None]
+    first = vars(od.od_token_logprobs(ctx, x, ids, T, n_top=n))
+    z = ((x.double() - x.double().max(2, keepdim=True).values) / T.double()[:, None, None]).squeeze(1)[peak]
+    rest = torch.exp(torch.where(z == 0, -INF, z)).sum(1)
+    assert torch.equal(z.argmax(1), at[peak])
+    same(first["logprob"][peak, 0], -torch.log1p(rest), 2.0 ** -16 * rest)
+    for _ in range(30):
+        again = vars(od.od_token_logprobs(ctx, x, ids, T, n_top=n))
+        assert all(torch.equal(first[k], again[k]) for k in first)
