@@ -457,7 +457,12 @@ int32_t od_token_logprobs_grad(od_ctx *ctx, int32_t B, int32_t R, int32_t vocab,
  *   w[v,h] = scales[v, h / group] * (code[v,h] - 8),
  *   logits[n,v] = sum_h hidden[n,h] w[v,h],   g_hidden[n,h] = sum_v g_logits[n,v] w[v,h].
  * Sums are fp32, nothing is rounded before them: a product of an input and a code is exact, scales
- * are applied to sums over a group (logits) or to the input (gradient, one fp32 rounding). Infinities
+ * are applied to sums over a group (logits) or to the input (gradient, one fp32 rounding). The
+ * tensor cores cut what they add, where an fp32 step would round it: against 64 bits results are
+ * about as far off as with plain fp32 sums or nearer, but for two cases that are up to some 1e-6 of
+ * the results' norm (1e-7 with plain sums): logits of bf16 hidden states that have one sign or a few
+ * columns far larger than the rest (8 x is taken off sums of x code), and a gradient written as
+ * bf16 (before its rounding). Infinities
  * and NaN of the inputs give what the formula gives; scales are finite. (Hidden states below 2^-90 of
  * their token's largest lose digits, as fp32's smallest numbers do.)
  *   in  (device) hidden / g_logits fp32 or bf16, N rows, row stride in elements, base and stride

@@ -8,13 +8,17 @@
 // of fp32 sums (and of an fp32 gradient times its scale). The scale of a group belongs to a row of the weights: forward
 // it multiplies the group's sum, backward, where rows are summed over, the gradient.
 //
-// For a few tokens the codes are all there is to move, and unpacking them is what competes with that. Forward nothing is
-// subtracted from a code and nothing or'ed to it: with no more than eight bits set a bf16 number is its bits times 2^-133 (in
+// For a few tokens the codes are all there is to move, and unpacking them is what competes with that. Forward, of bf16 inputs,
+// nothing is subtracted from a code and nothing or'ed to it: with no more than eight bits set a bf16 number is its bits times 2^-133 (in
 // the first binade too), so two masks, a shift and two masks make eight codes u, half of them as 16 u, ready for the tensor
 // pipe. The inputs are scaled by a power of two so that products are in fp32's range, and divided by 16 where they meet a
-// 16 u. The 8 is taken off in what a group's sum begins at, -8 times the sum of its inputs, which adds no more to the sum's
-// magnitudes than the codes do. (Eight tokens through 128256 x 4096: 59 us with 136 subtracted from bf16 numbers 128 + u,
-// 52 us so.)
+// 16 u. The 8 is taken off in what a group's sum begins at, -8 times the sum of its inputs, which is exact for inputs of 8 bits that
+// are not too far apart. (Eight tokens through 128256 x 4096, bf16 results: 52 us, and 62 with u - 8 as ordinary bf16 numbers.) What that
+// costs is digits where inputs have one sign or a few of them stand out, as sums run through numbers many times the result: against 64 bits
+// 0.9e-6 of the result's norm for inputs of one sign through 4096 columns in groups of 128 (plain fp32 sums 1.5e-7), 1.4e-6 for 16384.
+// For fp32 inputs such a beginning is rounded itself (2e-5 for equal ones, 1.6e-6 for one sign): their codes are made u - 8, as
+// ordinary numbers, and a group's sums begin at zero (1e-7, where plain fp32 sums are 4e-7 off). Beside three pieces that costs little (8 tokens
+// through 32000 x 2048: 17.4 us for 16.5, 6 through 128256 x 1024 30.1 for 28.3).
 // Operands go from registers into mma.sync: for tcgen05 they would be written to shared memory and read there at two
 // bytes a weight, 29 us of its bandwidth for 128256 x 2048, whose codes HBM brings in 21.
 //
@@ -179,25 +183,30 @@ struct Scales {
 // a token. XS: a block of threads keeps its tokens' inputs in shared memory as the words of the fragments, 16 bytes to a
 // lane; where they do not fit, they are read and cut again for every 16 rows.
 
-// The scale of a token whose largest magnitude has these bits is 2^k: 106 where that is from 2^-8 up to 2^20, as it is nearly
-// always, so that products are x u 2^-27; for others (all of zeros too) what brings the largest to 2^126. An input keeps all its
-// digits down to 2^-90 of its token's largest.
+// The scale of a token whose largest magnitude has these bits is 2^(CODES + k). Codes are 2^-CODES of themselves (of fp32 inputs
+// they are themselves), and k is 0 or, for products in fp32's range, -27 where that is from 2^-8 up to 2^20, as it is nearly
+// always; for others (all of zeros too) it brings the largest to 2^-7. An input keeps all its digits down to 2^-90 of its token's
+// largest.
+template <bool F32> constexpr int CODES = F32 ? 0 : 133;
 __device__ __forceinline__ bool usual(uint32_t largest) { return largest >= (127u - 8 << 23) && largest < (127u + 20 << 23); }
-__device__ __forceinline__ int scale_of_token(uint32_t largest) { return usual(largest) ? 106 : 253 - (int)(largest >> 23); }
+template <bool F32>
+__device__ __forceinline__ int scale_of_token(uint32_t largest) { return CODES<F32> + (usual(largest) ? F32 ? 0 : -27 : 120 - (int)(largest >> 23)); }
 // eight columns of a token (columns 8t .. 8t + 7 of a block) by this; a token with infinities or NaN is zero here
+template <bool F32>
 struct Token {
     float up, up2;                                         // the scale is their product
     __device__ __forceinline__ Token(uint32_t largest)
     {
-        const int k = largest < 0x7F800000u ? scale_of_token(largest) : 0, h = k / 2;
+        const int k = largest < 0x7F800000u ? scale_of_token<F32>(largest) : 0, h = k / 2;
         up = largest < 0x7F800000u ? __int_as_float((127 + h) << 23) : 0.f;
         up2 = __int_as_float((127 + k - h) << 23);
     }
 };
-// sums of a token back to its units: they are of products times 2^(k - 133)
+// sums of a token back to its units
+template <bool F32>
 __device__ __forceinline__ float scaled_back(float v, uint32_t largest)
 {
-    const int k = 133 - scale_of_token(largest), h = k / 2;
+    const int k = CODES<F32> - scale_of_token<F32>(largest), h = k / 2;
     return v * __int_as_float((127 + h) << 23) * __int_as_float((127 + k - h) << 23);
 }
 template <bool F32>
@@ -216,7 +225,7 @@ __device__ __forceinline__ void load_columns(const void *at, bool has, float (&x
 }
 // and the words of a lane's fragments
 template <int P>
-__device__ __forceinline__ void cut_columns(float (&x)[8], const Token &k, uint32_t (&b)[P][4])
+__device__ __forceinline__ void cut_columns(float (&x)[8], const Token<P == 3> &k, uint32_t (&b)[P][4])
 {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -225,7 +234,7 @@ __device__ __forceinline__ void cut_columns(float (&x)[8], const Token &k, uint3
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float f = i & 1 ? 0.0625f : 1.f;
+        const float f = P == 1 && i & 1 ? 0.0625f : 1.f;   // (meets 16 u)
         uint32_t c[P];
         pieces<P>(x[i] * f, x[i + 4] * f, c);
 #pragma unroll
@@ -295,11 +304,11 @@ __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
 
     // [group][8 tokens to a part]: what the group's sums begin at; [block of 32 columns][part][piece][lane]: the fragments
     float *const starts = (float *)(smem + F_WARPS * RING * WIDE_STAGE);
-    unsigned char *const inputs = (unsigned char *)(starts + n_groups * 8 * NT);
+    unsigned char *const inputs = (unsigned char *)(starts + (F32 ? 0 : n_groups * 8 * NT));
     auto prepare = [&](bool all_usual) {
         for (int i = warp; i < n_groups * NT; i += F_WARPS) {
             const int q = i % NT, n = n0 + q * 8 + g;
-            const Token k(all_usual ? 127u << 23 : largest_of[q * 8 + g]);
+            const Token<F32> k(all_usual ? 127u << 23 : largest_of[q * 8 + g]);
             float start = 0.f;
             uint32_t m = 0;
 #pragma unroll
@@ -312,15 +321,18 @@ __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
                     for (int c = 0; c < 8; ++c) m = max(m, __float_as_uint(x[c]) & 0x7FFFFFFFu);
                 uint32_t b[P][4];
                 cut_columns<P>(x, k, b);
+                if (!F32)
 #pragma unroll
-                for (int c = 0; c < 8; ++c) start = fmaf(x[c], -0x1p-126f * 0.0625f, start);   // -8 times 2^-133
+                    for (int c = 0; c < 8; ++c) start = fmaf(x[c], -0x1p-126f * 0.0625f, start);   // -8 times 2^-133
                 if constexpr (XS)
 #pragma unroll
                     for (int p = 0; p < P; ++p) ((uint4 *)inputs)[((blk * NT + q) * P + p) * 32 + lane] = make_uint4(b[p][0], b[p][1], b[p][2], b[p][3]);
             }
-            start += __shfl_xor_sync(0xFFFFFFFFu, start, 1);
-            start += __shfl_xor_sync(0xFFFFFFFFu, start, 2);
-            if (t == 0) starts[i * 8 + g] = start;
+            if (!F32) {
+                start += __shfl_xor_sync(0xFFFFFFFFu, start, 1);
+                start += __shfl_xor_sync(0xFFFFFFFFu, start, 2);
+                if (t == 0) starts[i * 8 + g] = start;
+            }
             if (all_usual) {
                 m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
                 m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
@@ -391,18 +403,22 @@ __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
                     } else {
                         float x[8];
                         load_columns<F32>(x_at[q] + (size_t)(s * WIDE + j) * 32 * IN_BYTES, n0 + q * 8 + g < A.N, x);
-                        cut_columns<P>(x, Token(largest(q * 8 + g)), b[q]);
+                        cut_columns<P>(x, Token<F32>(largest(q * 8 + g)), b[q]);
                     }
                     if (j % GB == 0) {
-                        const float2 v = begin_at[(j / GB * NT + q) * 4];
+                        const float2 v = F32 ? make_float2(0.f, 0.f) : begin_at[(j / GB * NT + q) * 4];
                         sum[q][0] = sum[q][2] = v.x; sum[q][1] = sum[q][3] = v.y;
                         if (P > 1) small[q][0] = small[q][1] = small[q][2] = small[q][3] = 0.f;
                     }
                 }
                 const uint32_t w0 = lds32((get + slot) ^ (j << 4)), w1 = lds32(((get + slot) ^ (j << 4)) + 8 * 128);
-                const uint32_t v0 = w0 >> 8, v1 = w1 >> 8;
-                const uint32_t a0[4] = {w0 & CODE, w1 & CODE, w0 & CODE16, w1 & CODE16};
-                const uint32_t a1[4] = {v0 & CODE, v1 & CODE, v0 & CODE16, v1 & CODE16};
+                const uint32_t v0 = w0 >> 8, v1 = w1 >> 8, k = A.bf16_128;
+                uint32_t a0[4] = {w0 & CODE, w1 & CODE, w0 & CODE16, w1 & CODE16};
+                uint32_t a1[4] = {v0 & CODE, v1 & CODE, v0 & CODE16, v1 & CODE16};
+                if (F32) {
+                    a0[0] = unpack<0>(w0, k); a0[1] = unpack<0>(w1, k); a0[2] = unpack<1>(w0, k); a0[3] = unpack<1>(w1, k);
+                    a1[0] = unpack<2>(w0, k); a1[1] = unpack<2>(w1, k); a1[2] = unpack<3>(w0, k); a1[3] = unpack<3>(w1, k);
+                }
 #pragma unroll
                 for (int q = 0; q < NT; ++q) {
 #pragma unroll
@@ -457,7 +473,7 @@ __global__ void __launch_bounds__(F_THREADS, 1) od_q4_kernel(const Q4Args A)
                 const int m = q * 8 + 2 * t + (k & 1), n = n0 + m, v = u * ROWS + g + (k >> 1) * 8;
                 if (n >= A.N || v >= V) continue;
                 const uint32_t l = largest(m);
-                store(A, n, v, l < 0x7F800000u ? scaled_back(total[q][k], l) : one_logit<F32>(A, n, v, 32 * GB));
+                store(A, n, v, l < 0x7F800000u ? scaled_back<F32>(total[q][k], l) : one_logit<F32>(A, n, v, 32 * GB));
             }
     }
     cp_wait<0>();
@@ -763,7 +779,7 @@ constexpr int SMEM_MOST = 226 * 1024;                      // (and a little of f
 template <int P, int NT, int GB, bool XS>
 Variant forward_kernel(int32_t H)
 {
-    const int rest = part_bytes<NT> + H / GB * NT + (XS ? H * 16 * NT * P : 0), stage = F_WARPS * WIDE_STAGE;
+    const int rest = part_bytes<NT> + (P == 3 ? 0 : H / GB * NT) + (XS ? H * 16 * NT * P : 0), stage = F_WARPS * WIDE_STAGE;
     if (!XS || rest + 3 * stage <= SMEM_MOST) return {od_q4_kernel<P, NT, GB, XS, 3>, rest + 3 * stage, 8 * NT, F_THREADS};
     return {od_q4_kernel<P, NT, GB, XS, XS ? 2 : 3>, rest + 2 * stage, 8 * NT, F_THREADS};
 }
