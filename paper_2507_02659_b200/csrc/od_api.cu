@@ -141,7 +141,6 @@ bool prepare_kernels(od_ctx *c)
     struct Resident {
         unsigned long long context;
         int32_t sample[OD_SAMPLE_LEVELS], step[OD_SAMPLE_LEVELS], shard[OD_SHARD_SIZES][OD_SAMPLE_MAX_PARTS + 1], distill[OD_DISTILL_LEVELS];
-        int32_t q4[OD_Q4_MAX_SPLIT + 1];
     };
     constexpr int DEVICES = 64;
     static std::mutex mutex;
@@ -152,15 +151,13 @@ bool prepare_kernels(od_ctx *c)
     const unsigned long long id = cuda_context_id();
     if (id == 0 || r.context != id) {
         r.context = 0;
-        if (od_sample_prepare_device(r.sample, r.shard) != cudaSuccess || od_step_prepare_device(r.step) != cudaSuccess ||
-            od_q4_prepare_device(r.q4) != cudaSuccess) return false;
+        if (od_sample_prepare_device(r.sample, r.shard) != cudaSuccess || od_step_prepare_device(r.step) != cudaSuccess) return false;
         od_distill_resident(r.distill);
         r.context = id;
     }
     memcpy(c->sample_clusters, r.sample, sizeof(r.sample));
     memcpy(c->step_clusters, r.step, sizeof(r.step));
     memcpy(c->shard_clusters, r.shard, sizeof(r.shard));
-    memcpy(c->q4_clusters, r.q4, sizeof(r.q4));
     memcpy(c->distill_few_clusters, r.distill, sizeof(r.distill));
     return true;
 }

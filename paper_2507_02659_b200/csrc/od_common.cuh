@@ -25,6 +25,7 @@
 
 #define OD_Q4_MAX_SPLIT 16          // blocks of a cluster that share the rows of a layer of 4-bit weights
 #define OD_Q4_PART_BYTES 16384      // scratch of a block of the gradient through 4-bit weights
+#define OD_Q4_VARIANTS 84           // kernels of a layer of 4-bit weights
 
 #define OD_DISTILL_LEVELS 4         // the distillation kernel cuts the draft ids into 1, 2, 4 or 8 chunks
 #define OD_DISTILL_MAX_CHUNKS 8     // (a portable cluster)
@@ -45,7 +46,10 @@ struct od_ctx {
     int32_t step_clusters[OD_SAMPLE_LEVELS];     // of the whole step in one launch: a multiprocessor to each block
     int32_t shard_clusters[OD_SHARD_SIZES][OD_SAMPLE_MAX_PARTS + 1];   // of a shard's mass, by threads and blocks
     int32_t distill_few_clusters[OD_DISTILL_LEVELS];   // of the distillation loss with two blocks to a multiprocessor
-    int32_t q4_clusters[OD_Q4_MAX_SPLIT + 1];          // of the gradient through 4-bit weights, by blocks
+    // of the gradient through 4-bit weights, by blocks, once it is asked for; and the kernels of the layer whose limits are set
+    int32_t q4_clusters[OD_Q4_MAX_SPLIT + 1];
+    const void *q4_kernels[OD_Q4_VARIANTS];
+    bool q4_clusters_known;
     bool have_map;
     bool distill_lists;             // some map had gather lists: every later one has the distillation kernel's
     // The map's serial number. A launch is laid out for the map of its time (where ids are shared, how many
@@ -323,9 +327,8 @@ cudaError_t od_launch_score_grad(const od_ctx *c, int32_t B, int32_t R, int32_t 
                                  const int32_t *top_ids, const float *g_logprob, const float *g_entropy, const float *g_top, void *grad,
                                  int64_t grad_row_stride, int64_t grad_seq_stride, cudaStream_t s);
 
-cudaError_t od_q4_prepare_device(int32_t *clusters);
 // an output layer with 4-bit weights: logits b of hidden states a, or (backward) their gradient b of the logits' a
-cudaError_t od_launch_q4(const od_ctx *c, bool backward, int32_t N, int32_t V, int32_t H, int32_t G, const void *a, int32_t a_dtype,
+cudaError_t od_launch_q4(od_ctx *c, bool backward, int32_t N, int32_t V, int32_t H, int32_t G, const void *a, int32_t a_dtype,
                          int64_t as, const void *codes, const void *scales, void *b, int32_t b_dtype, int64_t bs, cudaStream_t s);
 
 void od_cache_free_dynamic(od_ctx *c);   // frees what od_cache_configure allocated beyond keys / vals

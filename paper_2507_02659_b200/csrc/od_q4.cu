@@ -32,6 +32,8 @@
 // and 37 % backward).
 #include <float.h>
 
+#include <mutex>
+
 #include "od_common.cuh"
 
 namespace {
@@ -834,25 +836,50 @@ cudaError_t launch(K kernel, dim3 grid, dim3 threads, int smem, int cluster, boo
 
 }  // namespace
 
-// the kernels' limits; clusters[n]: clusters of n blocks of the gradient that are resident at a time
-cudaError_t od_q4_prepare_device(int32_t *clusters)
+// What a kernel needs is set when a context launches it for the first time, and what the gradient asks of the device when it is
+// called first: for all 84 kernels it took 23 ms in every process's first od_create, of those too that have no such layer. (Neither
+// allocates or waits: also while a stream is captured. Two threads may call at once.)
+namespace {
+
+std::mutex &first_calls() { static std::mutex m; return m; }
+
+bool limits_set(const od_ctx *c, const void *kernel)
 {
-    Kernel done = nullptr;
-    // (every variant: these sizes reach one, two, four parts of 8 tokens, rings of three and two stages, and none in shared memory)
-    for (int backward = 0; backward < 2; ++backward)
-        for (int32_t G = 32; G <= 128; G *= 2)
-            for (int types = 0; types < 4; ++types)
-                for (int N = 8; N <= 32; N += 8)
-                    for (int32_t H = 128; H <= 65536; H += H < 16384 ? 128 : 49152) {
-                        const Variant v = variant(backward, G, types & 1, types >> 1, N, H);
-                        if (v.kernel == done) continue;
-                        cudaError_t e = cudaFuncSetAttribute((const void *)v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST);
-                        if (e == cudaSuccess && backward) e = cudaFuncSetAttribute((const void *)v.kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-                        if (e != cudaSuccess) return e;
-                        done = v.kernel;
-                    }
-    for (int n = 0; n <= OD_Q4_MAX_SPLIT; ++n) {           // (the variant with the most shared memory; each fills a multiprocessor)
-        const Variant v = variant(true, 32, true, true, 8, 128);
+    for (const void *const &k : c->q4_kernels) {
+        const void *const known = __atomic_load_n(&k, __ATOMIC_ACQUIRE);
+        if (known == kernel) return true;
+        if (!known) break;
+    }
+    return false;
+}
+
+cudaError_t set_limits(od_ctx *c, const void *kernel, bool backward)
+{
+    if (limits_set(c, kernel)) return cudaSuccess;
+    std::lock_guard<std::mutex> lock(first_calls());
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MOST);
+    if (e == cudaSuccess && backward) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+    for (const void *&k : c->q4_kernels) {
+        if (k == kernel) break;
+        if (k) continue;
+        __atomic_store_n(&k, kernel, __ATOMIC_RELEASE);
+        break;
+    }
+    return cudaSuccess;
+}
+
+// q4_clusters[n]: clusters of n blocks of the gradient that are resident at a time, by the variant with the most shared memory
+// (each fills a multiprocessor)
+cudaError_t ask_for_clusters(od_ctx *c)
+{
+    if (__atomic_load_n(&c->q4_clusters_known, __ATOMIC_ACQUIRE)) return cudaSuccess;
+    const Variant v = variant(true, 32, true, true, 8, 128);
+    const cudaError_t e = set_limits(c, (const void *)v.kernel, true);
+    if (e != cudaSuccess) return e;
+    std::lock_guard<std::mutex> lock(first_calls());
+    if (c->q4_clusters_known) return cudaSuccess;
+    for (int n = 0; n <= OD_Q4_MAX_SPLIT; ++n) {
         cudaLaunchConfig_t cfg = {};
         cudaLaunchAttribute attr[1];
         attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -864,12 +891,15 @@ cudaError_t od_q4_prepare_device(int32_t *clusters)
             cudaGetLastError();
             here = 0;
         }
-        clusters[n] = here;
+        c->q4_clusters[n] = here;
     }
+    __atomic_store_n(&c->q4_clusters_known, true, __ATOMIC_RELEASE);
     return cudaSuccess;
 }
 
-cudaError_t od_launch_q4(const od_ctx *c, bool backward, int32_t N, int32_t V, int32_t H, int32_t G, const void *a, int32_t a_dtype,
+}  // namespace
+
+cudaError_t od_launch_q4(od_ctx *c, bool backward, int32_t N, int32_t V, int32_t H, int32_t G, const void *a, int32_t a_dtype,
                          int64_t as, const void *codes, const void *scales, void *b, int32_t b_dtype, int64_t bs, cudaStream_t s)
 {
     const bool f32 = a_dtype == OD_F32, pdl = c->opt_pdl != 0;
@@ -878,6 +908,8 @@ cudaError_t od_launch_q4(const od_ctx *c, bool backward, int32_t N, int32_t V, i
                    H % COLS == 0 && ((uintptr_t)scales & 7u) == 0, 0x43004300u, 1, 1, 1, 0, 0, c->d_q4_parts};
     if (!backward) {
         const Variant v = variant(false, G, f32, false, N, H);
+        const cudaError_t ready = set_limits(c, (const void *)v.kernel, false);
+        if (ready != cudaSuccess) return ready;
         const int64_t units = ((int64_t)V + ROWS - 1) / ROWS, blocks = units < sms ? units : sms;
         // Warps to the same 16 rows (1, 2, 4), by the time of a warp's turns: its stages, and for the sums to be joined as much as
         // one stage more, or of four warps three. (us, 1 / 2 / 4: 8 tokens through 128256 x 4096 59 / 52 / 57, 2000 x 4096
@@ -890,9 +922,13 @@ cudaError_t od_launch_q4(const od_ctx *c, bool backward, int32_t N, int32_t V, i
         }
         return launch(v.kernel, dim3((unsigned)blocks, (unsigned)((N + v.tokens - 1) / v.tokens)), F_THREADS, v.smem, 1, pdl, s, args);
     }
+    cudaError_t e = ask_for_clusters(c);
+    if (e != cudaSuccess) return e;
     // 32 tokens at a time, then what is left: the scratch is for one time
     for (int32_t n = 0; n < N;) {
         const Variant v = variant(true, G, f32, b_dtype == OD_F32, N - n, H);
+        e = set_limits(c, (const void *)v.kernel, true);
+        if (e != cudaSuccess) return e;
         // Warps side by side (4, 2, 1), blocks on the same columns (as many as there are multiprocessors for, or a cluster of
         // any size) and how these are joined, by the time that it takes in twentieths of a us, as measured with 16 warps (in proportion to them it chose no better): a stage of a warp 13, and
         // for every eight tokens 13, 6 for each group of its columns but one and 6 if they are fp32; the join 80, a cluster 20.
@@ -914,7 +950,7 @@ cudaError_t od_launch_q4(const od_ctx *c, bool backward, int32_t N, int32_t V, i
                 if (c->q4_clusters[k] > 0) offer(cw, k, (tiles + c->q4_clusters[k] - 1) / c->q4_clusters[k], 20, true);
         }
         args.first_token = n;
-        cudaError_t e = launch(v.kernel, dim3((unsigned)blocks), v.threads, v.smem, args.cluster ? args.split : 1, pdl, s, args);
+        e = launch(v.kernel, dim3((unsigned)blocks), v.threads, v.smem, args.cluster ? args.split : 1, pdl, s, args);
         if (e == cudaSuccess && args.split > 1 && !args.cluster)
             e = launch(od_q4_join_kernel, dim3((unsigned)(H / 32), (unsigned)(N - n < v.tokens ? N - n : v.tokens)), dim3(32, JOIN), 0, 1, pdl, s, args, v.tokens);
         if (e != cudaSuccess) return e;

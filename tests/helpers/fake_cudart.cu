@@ -17,6 +17,7 @@ namespace {
 
 std::map<const void *, std::string> &kernels() { static std::map<const void *, std::string> k; return k; }
 std::string &log_text() { static std::string s; return s; }
+std::string &limits_text() { static std::string s; return s; }
 struct Range { const char *p; size_t bytes; };
 std::vector<Range> &pinned() { static std::vector<Range> v; return v; }
 bool no_driver_functions = false;
@@ -70,6 +71,7 @@ extern "C" {
 
 // ---- for the tests
 const char *fake_log(void) { static std::string last; last = log_text(); log_text().clear(); return last.c_str(); }
+const char *fake_limits(void) { static std::string last; last = limits_text(); limits_text().clear(); return last.c_str(); }   // kernels whose attributes were set
 void fake_pin(const void *p, size_t bytes) { pinned().push_back({(const char *)p, bytes}); }
 void fake_unpin_all(void) { pinned().clear(); }
 void fake_no_driver_functions(int none) { no_driver_functions = none != 0; }
@@ -113,7 +115,7 @@ cudaError_t cudaMemcpyAsync(void *d, const void *s, size_t n, cudaMemcpyKind kin
     return cudaSuccess;
 }
 cudaError_t cudaMemset(void *p, int v, size_t n) { memset(p, v, n); return cudaSuccess; }
-cudaError_t cudaFuncSetAttribute(const void *, cudaFuncAttribute, int) { return cudaSuccess; }
+cudaError_t cudaFuncSetAttribute(const void *func, cudaFuncAttribute, int) { limits_text() += kernels()[func] + "\n"; return cudaSuccess; }
 cudaError_t cudaGetDevice(int *d) { *d = 0; return cudaSuccess; }
 cudaError_t cudaSetDevice(int) { return cudaSuccess; }
 cudaError_t cudaGetDeviceCount(int *n) { *n = 1; return cudaSuccess; }

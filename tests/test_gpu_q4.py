@@ -435,3 +435,33 @@ def test_inputs_of_one_sign(ctx, N, V, H, G, kind, dtype):
     want = x.double() @ weights(codes, scales).T
     got = od.od_q4_logits(ctx, x, codes, scales).double()
     assert float((got - want).norm() / want.norm()) <= 2.0 ** -19
+
+
+def test_the_first_calls_of_a_process_are_captured():
+    """What kernels need is set at their first launch: into a graph too."""
+    import os
+    import subprocess
+    import sys
+    program = """
+import torch
+from paper_2507_02659_b200 import binding as od
+ctx = od.Context("cuda:0", 10, 10, 1, 1)
+g = torch.Generator(device="cuda").manual_seed(1)
+V, H = 20003, 1024
+codes = torch.randint(0, 256, (V, H // 2), generator=g, device="cuda", dtype=torch.uint8)
+scales = torch.rand(V, H // 64, generator=g, device="cuda").bfloat16()
+for n, dtype in ((7, torch.bfloat16), (20, torch.float32), (40, torch.bfloat16)):
+    x = torch.randn(n, H, generator=g, device="cuda").to(dtype)
+    y, dx = torch.zeros(n, V // 4 * 4 + 4, device="cuda")[:, :V], torch.zeros(n, H, device="cuda", dtype=dtype)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        od.od_q4_logits(ctx, x, codes, scales, out=y)
+        od.od_q4_logits_grad(ctx, y, codes, scales, out=dx)
+    graph.replay()
+    want = od.od_q4_logits(ctx, x, codes, scales)
+    back = od.od_q4_logits_grad(ctx, want, codes, scales, dtype=dtype)
+    assert want.any() and back.any() and torch.equal(y, want) and torch.equal(dx, back), n
+ctx.close()
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run([sys.executable, "-c", program], check=True, cwd=root, timeout=300)

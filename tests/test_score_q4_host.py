@@ -156,3 +156,31 @@ def test_the_gradients_join(without_clusters):
     assert len(got) == 4 and all(b <= 148 and y == 1 for _, b, y in got[0::2])
     assert [x[1:] for x in got[1::2]] == [(2048 // 32, 32), (2048 // 32, 8)]
     lib.close()
+
+
+def test_kernels_of_the_layer_are_made_ready_when_they_are_first_launched():
+    """Not in od_create, which is everybody's; and once to a context."""
+    L = helpers.fake_runtime_lib()
+    L.fake_limits.restype = C.c_char_p
+    L.fake_no_driver_functions(1)                           # (od_create sets the limits of its kernels every time)
+    try:
+        L.fake_limits()
+        lib = Lib()
+        created = L.fake_limits().decode().split()
+        assert created and not [k for k in created if "od_q4" in k]
+        assert lib.scores() == OK and L.fake_limits() == b""
+        seen = set()
+        for kw in [dict(), dict(H=4096, N=30, V=1000), dict(dtype=F32), dict(G=64), dict(H=65536), dict(backward=True),
+                   dict(backward=True, N=40, V=20000, H=2048)]:
+            assert lib.q4(**kw) == OK
+            ready = set(L.fake_limits().decode().split())
+            assert ready and not ready & seen and all("od_q4" in k for k in ready), kw
+            assert lib.q4(**kw) == OK and L.fake_limits() == b"", kw
+            seen |= ready
+        other = Lib()
+        assert lib.q4() == OK and not [k for k in L.fake_limits().decode().split() if "od_q4" in k]
+        assert other.q4() == OK and [k for k in L.fake_limits().decode().split() if "od_q4" in k]
+        other.close()
+        lib.close()
+    finally:
+        L.fake_no_driver_functions(0)
