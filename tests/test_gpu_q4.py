@@ -465,3 +465,29 @@ ctx.close()
 """
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     subprocess.run([sys.executable, "-c", program], check=True, cwd=root, timeout=300)
+
+
+@pytest.mark.parametrize("given,made", TYPES)
+@pytest.mark.parametrize("N", [1, 8, 16, 24, 32, 40])
+@pytest.mark.parametrize("V,H,G", [(20011, 256, 32), (20003, 2048, 128), (30001, 1152, 64)])
+def test_gradients_through_long_layers(ctx, V, H, G, N, given, made):
+    """Errors of the whole, where the bound for single results lets some hundred rows go missing. A warp has at most every eighth 32
+    rows of its block, and blocks share the rows of these layers by 18 and more, up to 14 stages of 2 x 3 instructions: as fp32
+    steps to either side (2^-24 of the sum) they are off by 2^-20 of it and so is what joins 148 parts: 2^-19 of the norm. Cut by 2^-23
+    each and all to one side they are 2^-16 of the results' root mean square at a single one that is written as bf16."""
+    codes, scales = layer(V, H, G, 34)
+    w = weights(codes, scales)
+    g = torch.Generator(device="cuda").manual_seed(35)
+    dy = padded(torch.randn(N, V, generator=g, device="cuda").to(given))
+    want = dy.double() @ w
+    got = od.od_q4_logits_grad(ctx, dy, codes, scales, dtype=made).double()
+    if made == F32:
+        assert float((got - want).norm() / want.norm()) <= 2.0 ** -19
+    else:
+        same(got, want, HALF[BF16] * want.abs() + 2.0 ** -16 * want.square().mean().sqrt())
+    # rows at the ends of the layer and of stages alone: none of them is left out, nor counted twice
+    rows = torch.tensor([0, 15, 16, 31, 32, 255, 256, V // 64 * 32 - 1, V // 64 * 32, V // 32 * 32 - 33, V // 32 * 32 - 1, V // 32 * 32, V - 1], device="cuda")
+    for r in (rows, rows[-1:], rows[-2:-1]):
+        few = torch.zeros_like(dy)
+        few[:, r] = dy[:, r]
+        check_grad(od.od_q4_logits_grad(ctx, padded(few), codes, scales, dtype=made), few[:, r], w[r], magnitudes(codes[r], scales[r]))
