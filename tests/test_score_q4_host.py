@@ -184,3 +184,13 @@ def test_kernels_of_the_layer_are_made_ready_when_they_are_first_launched():
         lib.close()
     finally:
         L.fake_no_driver_functions(0)
+
+
+def test_refused_scores_launch_nothing(lib):
+    odd = lib.buffer(64, 2)
+    for kw in [dict(ctx=None), dict(B=-1), dict(R=0), dict(V=0), dict(n_top=33), dict(n_top=-1), dict(top_ids=None), dict(top_lp=None),
+               dict(logits=None), dict(row_max=None), dict(row_sum=None), dict(row=56), dict(seq=64), dict(B=1 << 20, R=1 << 20), dict(dtype=2),
+               dict(V=(1 << 30) + 8), dict(logits=odd), dict(row=65), dict(seq=197)]:
+        assert lib.scores(**kw) != OK, kw
+    assert lib.log() == []
+    assert lib.scores(n_top=0, top_ids=None, top_lp=None) == OK and len(lib.log()) == 1
