@@ -439,6 +439,10 @@ int32_t od_token_logprobs(od_ctx *ctx, int32_t B, int32_t R, int32_t vocab, cons
  *                r*grad_row_stride + t (alignment as for the logits); it may be the logits
  *                themselves, with the same strides. Rows that do not count, with a bad
  *                temperature or without mass are 0; nothing behind a row is written.
+ * p(t) is within some 2^-16 of its value. In a row with all but 2^-8 of its mass on one token that token's
+ * value is a difference of nearly equal numbers: within 2^-21 (sum_i |g_i| + |g_entropy|) / T of the formula's (before
+ * it is rounded to bf16) and no nearer, however small the formula's is; g_logprob (1 - p(t)) / T has no digits
+ * left where 1 - p(t) is below 2^-21, as with other fp32 probabilities (row_sum has no more of them).
  * Asynchronous on `stream`; no scratch. */
 int32_t od_token_logprobs_grad(od_ctx *ctx, int32_t B, int32_t R, int32_t vocab,
                                const void *logits, int32_t logit_dtype, int64_t row_stride,

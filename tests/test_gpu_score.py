@@ -507,3 +507,32 @@ def test_rows_with_nearly_all_mass_on_one_token_are_the_same_in_every_run(ctx, r
     for _ in range(30):
         again = vars(od.od_token_logprobs(ctx, x, ids, T, n_top=n))
         assert all(torch.equal(first[k], again[k]) for k in first)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,V", [(4, 33), (40, 32000), (300, 4099)])
+def test_gradients_of_rows_with_nearly_all_mass_on_one_token(ctx, rows, V, dtype):
+    """At that token within 2^-21 of the weights' magnitudes, as the header says: the row sum, its product with T, the quotient, two
+    products, sum / T and the difference are a rounding of 2^-24 each (of G + g_entropy (entropy - ln row_sum), where the
+    logarithm has 2^-23 of row_sum's own too, and entropies are below 0.01 here); elsewhere relative to p (G + g_entropy (ln p + entropy))."""
+    g = torch.Generator(device="cuda").manual_seed(20)
+    x = torch.randn(rows, 1, V, generator=g, device="cuda")
+    at = torch.randint(0, V, (rows,), generator=g, device="cuda")
+    x[torch.arange(rows), 0, at] = 16.0 + 10.0 * torch.rand(rows, generator=g, device="cuda")
+    x = padded(x.to(dtype))
+    T = torch.full((rows,), 0.7, device="cuda")
+    ids = at.int()[:, None]
+    ids[1::4] = (ids[1::4] + 1) % V                         # another token than the one with the mass
+    g_lp, g_h = torch.randn(rows, 1, generator=g, device="cuda"), torch.randn(rows, 1, generator=g, device="cuda")
+    g_top = torch.randn(rows, 1, 2, generator=g, device="cuda")
+    out = od.od_token_logprobs(ctx, x, ids, T, n_top=2)
+    ref = reference(x, ids, T, 2)
+    half = 2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -24
+    for a, b, c in [(g_lp, None, None), (g_lp, g_h, g_top), (None, g_h, None)]:
+        want, tol = grad_reference(x, ids, T, ref, a, b, c, 2)
+        weights = sum(t.double().abs().sum(2) if t.dim() == 3 else t.double().abs() for t in (a, b, c) if t is not None)
+        limit = (2.0 ** -21 * weights / T.double()[:, None])[:, :, None].expand_as(want)
+        named = torch.zeros_like(want, dtype=torch.bool).scatter_(2, at[:, None, None], True)
+        named.scatter_(2, ids.long()[:, :, None], True).scatter_(2, ref["top_ids"], True)
+        tol = torch.where(named, limit, tol)
+        same(od.od_token_logprobs_grad(ctx, x, ids, out, a, b, c, temperature=T), want, tol + half * (want.abs() + tol))
