@@ -250,3 +250,54 @@ def test_logits_may_be_written_directly_in_front(cuda_device, grid, B, call):
         for a, b in zip(want, got):
             assert torch.equal(a, b)
     ctx.close()
+
+
+@pytest.mark.parametrize("call", ["scores", "scores_few_rows", "scores_grad", "layer", "layer_grad", "layer_grad_joined"])
+def test_scores_and_the_layer_between_a_late_producer_and_a_translation(cuda_device, call):
+    """They read nothing before what is in front of them is done, and let what is behind them, which may read early, start no sooner."""
+    w = _workload(B=2, k_max=3)
+    st = synth.make_static(w)
+    ctx = parity.make_context(w, st, cuda_device)
+    s = synth.make_step(w, st, 0, device=cuda_device)
+    g = torch.Generator(device=cuda_device).manual_seed(1)
+    rows = torch.randn(*((1, 1, 152064) if call == "scores_few_rows" else (40, 5, 8000)), generator=g, device=cuda_device)
+    ids = torch.zeros(rows.shape[:2], dtype=torch.int32, device=cuda_device)
+    lp = od.od_token_logprobs(ctx, rows, ids, n_top=4)
+    one = torch.ones(rows.shape[:2], device=cuda_device)
+    out = od.alloc_logprob_out(ctx, *rows.shape[:2], 4)     # (nothing is launched but the call)
+    V, H = (20000, 1024) if call == "layer_grad_joined" else (5000, 256)
+    codes = torch.randint(0, 256, (V, H // 2), generator=g, device=cuda_device, dtype=torch.uint8)
+    scales = torch.rand(V, H // 64, generator=g, device=cuda_device).to(torch.bfloat16)
+    hidden, dy = (torch.randn(40, n, generator=g, device=cuda_device) for n in (H, V))
+    source, run = {
+        "scores": (rows, lambda x: list(vars(od.od_token_logprobs(ctx, x, ids, n_top=4, out=out)).values())),
+        "scores_few_rows": (rows, lambda x: list(vars(od.od_token_logprobs(ctx, x, ids, n_top=4, out=out)).values())),
+        "scores_grad": (rows, lambda x: [od.od_token_logprobs_grad(ctx, x, ids, lp, one, one)]),
+        "layer": (hidden, lambda x: [od.od_q4_logits(ctx, x, codes, scales)]),
+        "layer_grad": (dy, lambda x: [od.od_q4_logits_grad(ctx, x, codes, scales)]),
+        "layer_grad_joined": (dy, lambda x: [od.od_q4_logits_grad(ctx, x, codes, scales)]),
+    }[call]
+    want = [t.clone() for t in run(source)]
+    late = torch.empty_like(source)
+    for _ in range(4):
+        late.fill_(0)
+        torch.cuda.synchronize()
+        _produce(late, source)
+        got = run(late)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+    mapped = od.od_map_proposals(ctx, s.draft_ids, s.draft_len, s.q_sel)
+    n = s.draft_ids.numel()
+    proposal = torch.zeros(n + -n % 4, dtype=torch.int32, device=cuda_device)
+    proposal[:n] = s.draft_ids.flatten()
+    late_ids = torch.empty_like(proposal)
+    ctx.set_option("early_inputs", 1)
+    for _ in range(4):
+        late_ids.fill_(1)
+        torch.cuda.synchronize()
+        _produce(late_ids, proposal)
+        run(source)
+        mp = od.od_map_proposals(ctx, late_ids[:n].view(s.draft_ids.shape), s.draft_len, s.q_sel)
+        torch.cuda.synchronize()
+        assert torch.equal(mp.m, mapped.m) and torch.equal(mp.tail_kind, mapped.tail_kind)
+    ctx.close()
