@@ -396,12 +396,14 @@ int32_t od_distill_loss(od_ctx *ctx, int32_t B, int32_t K_max, const float *q_ro
 
 /* The log probability of one given token, the entropy and the likeliest tokens of each
  * logit row: what a server returns beside the tokens that it verified, and what a loss on
- * likelihood or entropy is made of. Of either model: `vocab` is the length of a row (any,
- * not bound to the context's vocabularies), B and R are not bound to its batch; no
+ * likelihood or entropy is made of. Of either model: `vocab` is the length of a row (at most
+ * 2^30, not bound to the context's vocabularies), B and R are not bound to its batch; no
  * vocabulary map is needed. Row (b, r), p = softmax(x / T_b):
  *   logprob = ln p(ids[b,r]); entropy = -sum_t p(t) ln p(t);
  *   top_ids, top_logprobs = the n_top largest logits in order, equal ones by the lower id.
- * A row is read once (its largest elements are looked at again).
+ * A row is read once, and of it again what holds its largest elements: in a row with nearly all mass
+ * on one token what the thread with that token has read, and where very many logits are equal, or most of
+ * the largest lie in one thread's elements, all of it.
  *   in  (device) logits  fp32 or bf16, element (b, r, t) at b*seq_stride + r*row_stride + t
  *                        (strides in elements; base and both strides multiples of 16 bytes);
  *                        nothing beyond a row's vocab elements is read
@@ -477,7 +479,7 @@ int32_t od_token_logprobs_grad(od_ctx *ctx, int32_t B, int32_t R, int32_t vocab,
  *                       otherwise) and hidden_size a multiple of it, at most 65536
  *   out (device) logits / g_hidden fp32 or bf16, N rows, base and stride multiples of 16 bytes;
  *                nothing behind a row is written
- * Neither vocab nor N is bound to the context. Made for N up to some dozens of tokens: the weights are
+ * Neither vocab (at most 2^30) nor N (at most 65535) is bound to the context. Made for N up to some dozens of tokens: the weights are
  * unpacked again for every few of them. Asynchronous on `stream`, allocates nothing, the same results
  * in every run. od_q4_logits_grad joins its sums in the context's scratch: it is ordered with the
  * other calls of its kind on the context like the step functions (graphs that hold it too);

@@ -20,16 +20,17 @@
 // ordinary numbers, and a group's sums begin at zero (1e-7, where plain fp32 sums are 4e-7 off). Beside three pieces that costs little (8 tokens
 // through 32000 x 2048: 17.4 us for 16.5, 6 through 128256 x 1024 30.1 for 28.3).
 // Operands go from registers into mma.sync: for tcgen05 they would be written to shared memory and read there at two
-// bytes a weight, 29 us of its bandwidth for 128256 x 2048, whose codes HBM brings in 21.
+// bytes a weight, 29 us of its bandwidth for 128256 x 2048 by arithmetic, whose codes HBM brings in 21. That speaks against it for 8
+// tokens; for 16 and more, where these kernels take 63 us and more backward, it does not, and tcgen05 has not been tried.
 //
 // A warp streams its own codes through a ring in shared memory (cp.async, 2 KB stages), so that no block barrier holds it
 // up: without the arithmetic the forward kernel reads 6.2 TB/s. Sixteen-byte pieces are placed so that the words of a
 // fragment lie in different banks.
 //
 // Measured (us; codes and scales / HBM's rate): forward 8 tokens, 128256 x 4096 in groups of 128: 52 (42), and 60 in a long
-// run, under the power cap; backward 8 positions, 128256 x 2048: 44 (21), 16: 63, 24: 85, 32: 105, with fp32 results 47, 71, 103 and 115. What bounds both
-// now is issue: masks share their dispatch with the matrix instructions (ncu: masks' pipe 56 %, tensor pipe 30 % forward; 56 %
-// and 37 % backward).
+// run, under the power cap; backward 8 positions, 128256 x 2048: 44 (21), 16: 63, 24: 85, 32: 105, with fp32 results 47, 71, 103 and 115. No
+// unit is full (ncu, 8 tokens): forward shared memory's data path is busiest, 67 %, as a warp reads 512 bytes of fragments for every 256
+// of codes, then issue 60 %, the masks' pipe 56 %, the tensor pipe 30 %; backward issue 61 %, the masks' pipe 56 %, the tensor pipe 37 %.
 #include <float.h>
 
 #include <mutex>

@@ -13,14 +13,16 @@
 // The alternatives cost next to nothing in that pass: the largest logits of 32 groups of threads are 32 different
 // elements, so the n-th largest of them is a bound that at least n elements of the slice reach and few more do. Threads leave
 // the maximum of every four loads in shared memory: only loads whose maximum reaches the bound are looked at again (from L2,
-// all of them at once), and what reaches the bound is ranked by counting.
+// all of them at once), and what reaches the bound is ranked by counting. Where too much reaches it (many equal logits, or many of
+// the largest in one thread's elements) each warp goes through its share of the slice again and keeps a sorted list. And where one token has nearly
+// all of the mass, what its thread has read is summed again without it.
 //
 // Backward: elementwise, one read and one write; the given token and the alternatives are written over the dense
 // values of their chunk behind a block barrier.
 //
-// Measured (us; HBM's rate for the bytes): scores of 4608 rows of 152064 bf16 logits with one alternative 242 (217), without
+// Measured (us; HBM's rate for the bytes): scores of 4608 rows of 152064 bf16 logits with one alternative 242 (213), without
 // 226; 96 rows of 128256 with 20 16 (3.8: launch, a row's chain of barriers, its alternatives); gradient of 448 rows of 128256,
-// 256 of which count, 32 (28). The large ones are at HBM's rate but for a row's end, the small ones at their chain.
+// 256 of which count, 32 (27). The large ones are at HBM's rate but for a row's end, the small ones at their chain.
 #include <float.h>
 
 #include "od_common.cuh"
