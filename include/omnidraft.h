@@ -465,10 +465,10 @@ int32_t od_token_logprobs_grad(od_ctx *ctx, int32_t B, int32_t R, int32_t vocab,
  * Sums are fp32, nothing is rounded before them: a product of an input and a code is exact, scales
  * are applied to sums over a group (logits) or to the input (gradient, one fp32 rounding). The
  * tensor cores cut what they add, where an fp32 step would round it: against 64 bits results are
- * about as far off as with plain fp32 sums or nearer, but for two cases that are up to some 1e-6 of
- * the results' norm (1e-7 with plain sums): logits of bf16 hidden states that have one sign or a few
- * columns far larger than the rest (8 x is taken off sums of x code), and a gradient written as
- * bf16 (before its rounding). Infinities
+ * about as far off as with plain fp32 sums or nearer, but for two cases: logits of bf16 hidden states that
+ * have one sign or a few columns far larger than the rest (8 x is taken off sums of x code; 1e-6 of the results'
+ * norm, up to 3e-6 in the longest rows, where plain sums are some 1e-7 off), and a gradient written as bf16
+ * (before its rounding, a hundredth of it at most: 3e-6 of the norm with 2048 columns, up to 3e-5 with 16384). Infinities
  * and NaN of the inputs give what the formula gives; scales are finite. (Hidden states below 2^-90 of
  * their token's largest lose digits, as fp32's smallest numbers do.)
  *   in  (device) hidden / g_logits fp32 or bf16, N rows, row stride in elements, base and stride
