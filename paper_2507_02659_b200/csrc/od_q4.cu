@@ -507,7 +507,7 @@ template <int P, int NT, int GB> constexpr int g_warp = G_RING * g_stage<P, NT> 
 // EXACT, for fp32 results: the tensor pipe cuts what it adds to its accumulators (to 2^-23 of the largest), so what it adds up in a
 // stage begins at zero and is then added to the sums in fp32 as such, which rounds (128256 x 1824, 28 positions: 2e-6 of the
 // result otherwise, where plain fp32 sums are 7e-7 off). For bf16 results it is left out: 20 % of the time with 24 positions, for cuts that add up
-// to 3e-5 of the result at most (152064 x 16384, 16 to 32 positions: all rows to eight warps), where its rounding is 2e-3.
+// to 3e-5 of the result at most (152064 x 16384, 24 or 32 positions: all rows to eight warps), where its rounding is 2e-3.
 template <int P, int NT, int GB, bool EXACT, int WARPS>
 __global__ void __launch_bounds__(32 * WARPS, 1) od_q4_grad_kernel(const Q4Args A)
 {
